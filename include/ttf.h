@@ -300,6 +300,118 @@ static inline double ttf_reduction_ratio(long long P, int F, int N) {
 }
 
 /*
+ * From the compressed clip to the model's attention.  (The paper leaves this to the language model: X' is projected to
+ * queries, keys and values, which are rotated by P' (Eq. compress_pos), kept in the cache that prefill builds and
+ * decoding extends (Eqs. Lpre, decode_pos), and in the streaming form "appended to the KV cache" (Discussion D3).)
+ * These entry points take what ttf_compress hands out as it hands it out: positions as int32 rows, the number of rows on
+ * the device, buffers of worst-case capacity whose rows beyond that number are neither read nor written.
+ *
+ * Like the rest of the library they only enqueue work and are deterministic; they use no scratch at all, so that calls on
+ * different streams and captured graphs share nothing.  Sums, softmax statistics and accumulators are fp32, results are
+ * rounded once.  Inputs may not overlap outputs except where stated.
+ */
+
+/* The heads of a sequence of rows: element d of head h of row i is data[i * row_stride + h * head_stride + d] (strides in
+ * elements, so that heads may be a part of a wider row, as in the output of one projection).  In an input of a call the
+ * memory is only read. */
+typedef struct {
+    void* data;
+    long long row_stride, head_stride;
+    int heads;
+} ttf_heads;
+
+/* Norm and rotation of a head x of D channels of the row at position p:
+ *   y = x * weight / sqrt(mean(x^2) + eps)                         (y = x where the weight is NULL)
+ *   for pair j < rot_dim / 2 with the angle p[axis(j)] * freq[j]:
+ *     (u, v) = (y[j], y[j + rot_dim / 2]), or (y[2j], y[2j + 1]) where interleaved
+ *     (u, v) -> factor * (u cos - v sin, v cos + u sin)
+ *   channels from rot_dim on: y.
+ * The table of frequencies carries any scaling for long contexts; factor is the attention factor of such scalings.  The
+ * angle is formed and reduced in 64 bits, so that far positions keep their turns.  With axes = 2 or 3 coordinates per
+ * position, section[a] pairs turn with coordinate a: in consecutive blocks (axis 0 first; the sections add up to
+ * rot_dim / 2), or with cyclic = 1 pair j with coordinate j mod axes while j / axes < section[that axis], else with 0. */
+typedef struct {
+    const float* freq;               /* [rot_dim / 2], device                                                          */
+    int rot_dim;                     /* channels that are rotated: even, 0 to D                                        */
+    int interleaved;                 /* 0: pairs half a rotation apart; 1: neighbouring channels                       */
+    int axes;                        /* coordinates per position, 1 to 3                                               */
+    int section[3];                  /* ignored for axes = 1                                                           */
+    int cyclic;
+    float factor;                    /* finite; 1 for none                                                             */
+    const void* q_weight;            /* [D] device, the heads' dtype; NULL: no norm of the queries                     */
+    const void* k_weight;            /* the same for the keys                                                          */
+    float eps;                       /* >= 0                                                                           */
+} ttf_rotation;
+
+/* A paged cache of keys and values: element d of head h of row r of page g is k[g * k_page + r * k_row + h * k_head + d]
+ * (strides in elements; both [pages, page_size, heads, D] and [pages, heads, page_size, D] are such layouts, and so are
+ * keys and values interleaved in one array).  Offsets may pass 32 bits. */
+typedef struct {
+    void* k;
+    void* v;
+    long long k_page, k_row, k_head, v_page, v_row, v_head;
+    int pages, page_size, heads, head_dim;
+    int dtype;                       /* a ttf_dtype                                                                    */
+} ttf_cache;
+
+/* The sequences of a call.  Rows [start[b], start[b + 1]) of the packed inputs are the new tokens of sequence b (none is
+ * allowed); they are the last ones of its length[b] cached tokens, so row i has slot length[b] - start[b + 1] + i.  Slot s
+ * lies in page table[b * table_stride + s / page_size], row s % page_size.  All three arrays are device memory and are read
+ * by the kernels: lengths may be results of earlier work on the stream (L' of ttf_compress among them).  Rows at or beyond
+ * start[seqs] are left as they are.  A sequence whose rows do not lie in [0, rows], whose length is negative or beyond
+ * table_pages pages, and a page that is needed and not in [0, pages), never make a kernel leave its arrays: ttf_paged_status
+ * tells TTF_ERR_BOUNDS, and the outputs and new cache rows of that sequence are undefined.  Entries of the table that no
+ * slot below length[b] needs may hold anything.  Tokens that lie before the cache (length[b] below the number of new rows)
+ * have no slot: they are not stored and see nothing. */
+typedef struct {
+    const int* start;                /* [seqs + 1]                                                                     */
+    const int* length;               /* [seqs]                                                                         */
+    const int* table;                /* [seqs, table_pages]                                                            */
+    long long table_stride;          /* elements between the rows of the table                                         */
+    int table_pages;
+    int seqs;
+    int rows;                        /* capacity of the packed arrays                                                  */
+} ttf_sequences;
+
+/*
+ * Norm and rotation of queries and keys in one pass.  q and k: inputs (either may be NULL, not both); out_q, out_k: outputs
+ * of the same number of heads, each either disjoint from its input or the same memory with the same strides.  positions
+ * int32 [rows, axes].  count: one int32 on the device, the rows that are there (at most `rows`; NULL: all).  head_dim 1 to
+ * 256, dtype a ttf_dtype.
+ */
+int ttf_rotate(const ttf_heads* q, const ttf_heads* k, int head_dim, int dtype, int rows, const int* count,
+               const int* positions, const ttf_rotation* rotation, const ttf_heads* out_q, const ttf_heads* out_k,
+               ttf_stream_t stream);
+
+/*
+ * Appends the new rows' keys and values to the cache: keys normed and rotated on the way, values as they are, and with q
+ * and out_q (both or neither) the queries normed and rotated into out_q by the same kernel.  rotation may be NULL: keys are
+ * stored as they come (q must then be NULL; positions are not read).  No two rows of a call may have the same slot of the
+ * same page.
+ */
+int ttf_cache_append(const ttf_heads* k, const ttf_heads* v, const ttf_heads* q, const int* positions,
+                     const ttf_rotation* rotation, const ttf_sequences* sequences, const ttf_cache* cache,
+                     const ttf_heads* out_q, ttf_stream_t stream);
+
+/*
+ * Attention of the new rows over the cache, which holds their own keys and values already (ttf_cache_append first):
+ *   out[i, h] = sum over the visible slots s of softmax_s(scale * <q[i, h], k[s, h / group]>) v[s, h / group]
+ * with group = q->heads / cache->heads (a whole number).  Row i at slot c sees every slot of its sequence with causal = 0,
+ * the slots up to c with causal = 1, of these only those above c - window where window > 0.  A row that sees nothing is
+ * zero.  Slots that no row of the sequence sees may hold anything, NaN included.  One row per sequence (decoding) to
+ * thousands (prefill, segments) in any mixture; the kernel is chosen by the sizes that the host knows.  head_dim 1 to 256.
+ */
+int ttf_attend(const ttf_heads* q, const ttf_sequences* sequences, const ttf_cache* cache, float scale, int causal,
+               int window, const ttf_heads* out, ttf_stream_t stream);
+
+/*
+ * Device-side status of ttf_rotate, ttf_cache_append and ttf_attend: waits for `stream`, then stores in *host_status the
+ * worst of what any of these calls has reported on the current device since the last query, and clears it: TTF_OK,
+ * TTF_ERR_TIMEOUT (a kernel gave up on a bounded wait; its outputs are undefined) or TTF_ERR_BOUNDS (see ttf_sequences).
+ */
+int ttf_paged_status(ttf_stream_t stream, int* host_status);
+
+/*
  * The same pass for callers whose tensors live in HOST memory (all four pointers are host pointers; pinned
  * memory makes the copies asynchronous).  Copies features to the device, runs ttf_compress, copies L' and the
  * first L' rows of tokens and positions back, and returns after synchronising.  Device staging buffers are

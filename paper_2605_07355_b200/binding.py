@@ -25,6 +25,7 @@ EXPORTS = [
     "ttf_query_static", "ttf_compress_ex", "ttf_query_ex", "ttf_compress_segment", "ttf_restore",
     "ttf_sim_histogram", "ttf_stats", "ttf_compress_batch", "ttf_compress_batch_ex", "ttf_profile_stages", "ttf_profile_read_floor", "ttf_compress_mean", "ttf_compress_host_batch",
     "ttf_set_schedule", "ttf_set_match_kernel", "ttf_last_device_status", "ttf_workspace_status", "ttf_debug_set_wait", "ttf_debug_func_attr_needed", "ttf_debug_set_check_slack", "ttf_debug_match_split",
+    "ttf_rotate", "ttf_cache_append", "ttf_attend", "ttf_paged_status",
 ]
 TTF_ERR_TIMEOUT, TTF_ERR_STATIC_LIMIT, TTF_ERR_BOUNDS = 5, 6, 7
 TTF_ANCHOR_AUTO, TTF_ANCHOR_FIRST, TTF_ANCHOR_LAST, TTF_ANCHOR_EXPLICIT = 0, 1, 2, 3
@@ -37,6 +38,32 @@ class TTFOptions(ctypes.Structure):
     _fields_ = [("anchor_mode", ctypes.c_int), ("anchor_frame", ctypes.c_int), ("order", ctypes.c_int),
                 ("pos_base", ctypes.c_int)]
 
+class TTFHeads(ctypes.Structure):
+    """ttf_heads of include/ttf.h"""
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_longlong), ("head_stride", ctypes.c_longlong),
+                ("heads", ctypes.c_int)]
+
+
+class TTFRotation(ctypes.Structure):
+    """ttf_rotation of include/ttf.h"""
+    _fields_ = [("freq", ctypes.c_void_p), ("rot_dim", ctypes.c_int), ("interleaved", ctypes.c_int), ("axes", ctypes.c_int),
+                ("section", ctypes.c_int * 3), ("cyclic", ctypes.c_int), ("factor", ctypes.c_float),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float)]
+
+
+class TTFCache(ctypes.Structure):
+    """ttf_cache of include/ttf.h"""
+    _fields_ = ([("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] +
+                [(n, ctypes.c_longlong) for n in ("k_page", "k_row", "k_head", "v_page", "v_row", "v_head")] +
+                [(n, ctypes.c_int) for n in ("pages", "page_size", "heads", "head_dim", "dtype")])
+
+
+class TTFSequences(ctypes.Structure):
+    """ttf_sequences of include/ttf.h"""
+    _fields_ = [("start", ctypes.c_void_p), ("length", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_longlong), ("table_pages", ctypes.c_int), ("seqs", ctypes.c_int),
+                ("rows", ctypes.c_int)]
+
 
 TTF_STATIC_SCRATCH_BYTES = 8 << 20
 KERNEL_KINDS = ["norm_sum", "frame_stats", "match", "compact", "fuse_count"]     # (the last: no kernel any more, always zero)
@@ -44,7 +71,8 @@ KERNEL_KINDS = ["norm_sum", "frame_stats", "match", "compact", "fuse_count"]    
 _lib = None
 _fast = None                     # _marshal, bound to the library's functions
 _FAST_FUNCTIONS = ["ttf_compress", "ttf_compress_ws", "ttf_compress_ex", "ttf_compress_segment", "ttf_compress_batch",
-                   "ttf_compress_batch_ex", "ttf_query", "ttf_query_ws", "ttf_query_ex", "ttf_restore", "ttf_stats"]
+                   "ttf_compress_batch_ex", "ttf_query", "ttf_query_ws", "ttf_query_ex", "ttf_restore", "ttf_stats",
+                   "ttf_rotate", "ttf_cache_append", "ttf_attend"]
 
 
 class TTFError(RuntimeError):
@@ -123,6 +151,14 @@ def lib() -> ctypes.CDLL:
         L.ttf_query_static.argtypes = [vp] + shape + [f, i, vp, vp, vp, vp, vp, vp]
         L.ttf_compress_host.restype = i
         L.ttf_compress_host.argtypes = [vp] + shape + [f, i, vp, vp, vp]
+        L.ttf_rotate.restype = i
+        L.ttf_rotate.argtypes = [vp, vp, i, i, i, vp, vp, vp, vp, vp, vp]
+        L.ttf_cache_append.restype = i
+        L.ttf_cache_append.argtypes = [vp] * 9
+        L.ttf_attend.restype = i
+        L.ttf_attend.argtypes = [vp, vp, vp, f, i, i, vp, vp]
+        L.ttf_paged_status.restype = i
+        L.ttf_paged_status.argtypes = [vp, ctypes.POINTER(i)]
         L.ttf_release.restype = i
         L.ttf_release.argtypes = []
         L.ttf_profile_begin.restype = i
@@ -562,6 +598,211 @@ def ttf_compress_host_batch(features, r: int, t: float, out_tokens=None, out_pos
         raise TTFError(rc, "ttf_compress_host_batch")
     Ls = [int(c) for c in counts]
     return [o[:L] for o, L in zip(out_tokens, Ls)], Ls, [o[:L] for o, L in zip(out_pos_thw, Ls)]
+
+
+_NO_HEADS = (0, 0, 0, 0)
+
+
+def _heads(name: str, x: Optional[torch.Tensor], like: torch.Tensor):
+    """[rows, heads, channels] of the device, dtype, rows and channels of `like` -> address, strides, number of heads"""
+    if x is None:
+        return _NO_HEADS
+    shape, of = x.shape, like.shape
+    if len(shape) != 3 or shape[0] != of[0] or shape[2] != of[2]:
+        raise ValueError(f"{name} must be [rows, heads, channels] = [{of[0]}, *, {of[2]}], got {tuple(shape)}")
+    if x.dtype != like.dtype or x.device != like.device:
+        raise ValueError(f"{name} must be {like.dtype} on {like.device}, got {x.dtype} on {x.device}")
+    row, head, channel = x.stride()
+    if channel != 1 and shape[2] > 1:
+        raise ValueError(f"the channels of {name} must be contiguous")
+    return x.data_ptr(), row, head, shape[1]
+
+
+def _out_heads(name: str, out: Optional[torch.Tensor], x: torch.Tensor, like: torch.Tensor):
+    """the output that goes with x: as given, or new"""
+    if out is None:
+        out = x.new_empty(x.shape)
+    elif out.shape != x.shape:
+        raise ValueError(f"{name} must have the shape of its input, {tuple(x.shape)}, got {tuple(out.shape)}")
+    return out, _heads(name, out, like)
+
+
+def _ints(name: str, x: torch.Tensor, dims: int, like: torch.Tensor) -> int:
+    if x.dtype != torch.int32 or x.dim() != dims or x.device != like.device:
+        raise ValueError(f"{name} must be an int32 tensor of {dims} dimensions on {like.device}, got {x.dtype}, {x.dim()} on {x.device}")
+    if dims == 1 and x.stride(0) != 1 and x.shape[0] > 1:
+        raise ValueError(f"{name} must be contiguous")
+    return x.data_ptr()
+
+
+def _rotation(positions, freq, q_weight, k_weight, rot_dim, interleaved, sections, cyclic, factor, eps, like):
+    """positions' address and the fields of ttf_rotation"""
+    rows, dim = like.shape[0], like.shape[2]
+    if positions.dim() == 1:
+        positions = positions.unsqueeze(1)
+    pos = _ints("positions", positions, 2, like)
+    axes = positions.shape[1]
+    if positions.shape[0] != rows or not positions.is_contiguous():
+        raise ValueError(f"positions must be contiguous [rows] or [rows, axes] with {rows} rows")
+    rot = dim if rot_dim is None else int(rot_dim)
+    if freq.dtype != torch.float32 or freq.device != like.device or freq.numel() != rot // 2 or not freq.is_contiguous():
+        raise ValueError(f"freq must hold {rot // 2} contiguous float32 values on {like.device}")
+    for w in (q_weight, k_weight):
+        if w is not None and (w.dtype != like.dtype or w.device != like.device or w.numel() != dim or not w.is_contiguous()):
+            raise ValueError(f"a norm's weight must hold {dim} contiguous {like.dtype} values on {like.device}")
+    if sections is None:
+        if axes != 1:
+            raise ValueError("positions with several coordinates need sections")
+        sections = (0, 0, 0)
+    elif len(sections) != axes:
+        raise ValueError(f"one section per coordinate: {axes}, got {len(sections)}")
+    else:
+        sections = (tuple(sections) + (0, 0))[:3]
+    return pos, (freq.data_ptr(), rot, 1 if interleaved else 0, axes, *sections, 1 if cyclic else 0, factor,
+                 _addr(q_weight), _addr(k_weight), eps)
+
+
+_NO_ROTATION = (0, 0, 0, 1, 0, 0, 0, 0, 1.0, 0, 0, 0.0)
+
+
+def ttf_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor, freq: torch.Tensor, *,
+               q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+               rot_dim: Optional[int] = None, interleaved: bool = False, sections=None, cyclic: bool = False,
+               factor: float = 1.0, count: Optional[torch.Tensor] = None, out_q: Optional[torch.Tensor] = None,
+               out_k: Optional[torch.Tensor] = None, stream=None):
+    """ttf_rotate: norm (where there is a weight) and rotation of the heads of q and k [rows, heads, channels] (either may be
+    None) by positions int32 [rows] or [rows, axes]; freq float32 [rot_dim / 2].  Only the first `count` rows (int32[1] on the
+    device; None: all) are read and written.  Returns (out_q, out_k); out_q may be q itself.  Does not synchronise."""
+    like = q if q is not None else k
+    if like is None:
+        raise ValueError("q or k must be given")
+    if not like.is_cuda:
+        raise ValueError(f"q and k must be CUDA tensors, got one on {like.device}")
+    there = _elsewhere(like)
+    if there is not None:
+        with there:
+            return ttf_rotate(q, k, positions, freq, q_weight=q_weight, k_weight=k_weight, eps=eps, rot_dim=rot_dim,
+                              interleaved=interleaved, sections=sections, cyclic=cyclic, factor=factor, count=count,
+                              out_q=out_q, out_k=out_k, stream=stream)
+    qh, kh = _heads("q", q, like), _heads("k", k, like)
+    oq = ok = _NO_HEADS
+    if q is not None:
+        out_q, oq = _out_heads("out_q", out_q, q, like)
+    elif out_q is not None:
+        raise ValueError("out_q without q")
+    if k is not None:
+        out_k, ok = _out_heads("out_k", out_k, k, like)
+    elif out_k is not None:
+        raise ValueError("out_k without k")
+    pos, rotation = _rotation(positions, freq, q_weight, k_weight, rot_dim, interleaved, sections, cyclic, factor, eps, like)
+    rows, _, dim = like.shape
+    cnt = 0 if count is None else _ints("count", count.reshape(-1), 1, like)
+    if rows == 0:
+        return out_q, out_k
+    rc = (_fast or _marshal()).rotate(*qh, *kh, dim, _dtype_code(like), rows, cnt, pos, *rotation, *oq, *ok,
+                                      _stream_of(like, stream))
+    if rc != TTF_OK:
+        raise TTFError(rc, "ttf_rotate")
+    return out_q, out_k
+
+
+def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, like: torch.Tensor):
+    shape = k_cache.shape
+    if len(shape) != 4 or v_cache.shape != shape or shape[3] != like.shape[2]:
+        raise ValueError(f"k_cache and v_cache must be [pages, page_size, heads, {like.shape[2]}], got {tuple(shape)} and {tuple(v_cache.shape)}")
+    for c in (k_cache, v_cache):
+        if c.dtype != like.dtype or c.device != like.device:
+            raise ValueError(f"the cache must be {like.dtype} on {like.device}, got {c.dtype} on {c.device}")
+    ks, vs = k_cache.stride(), v_cache.stride()
+    if (ks[3] != 1 or vs[3] != 1) and shape[3] > 1:
+        raise ValueError("the channels of the cache must be contiguous")
+    return (k_cache.data_ptr(), ks[0], ks[1], ks[2], v_cache.data_ptr(), vs[0], vs[1], vs[2], *shape, _dtype_code(like))
+
+
+def _sequences(start: torch.Tensor, length: torch.Tensor, table: torch.Tensor, like: torch.Tensor):
+    s, n, t = _ints("start", start, 1, like), _ints("length", length, 1, like), _ints("table", table, 2, like)
+    seqs, pages = table.shape
+    if start.shape[0] != seqs + 1 or length.shape[0] != seqs:
+        raise ValueError(f"a table of {seqs} sequences goes with {seqs + 1} starts and {seqs} lengths, got {start.shape[0]} and {length.shape[0]}")
+    if pages > 1 and table.stride(1) != 1:
+        raise ValueError("the rows of the table must be contiguous")
+    return s, n, t, (table.stride(0) if seqs > 1 else pages), pages, seqs, like.shape[0]
+
+
+def ttf_cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, start: torch.Tensor,
+                     length: torch.Tensor, table: torch.Tensor, positions: Optional[torch.Tensor] = None,
+                     freq: Optional[torch.Tensor] = None, *, q: Optional[torch.Tensor] = None,
+                     out_q: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                     k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, rot_dim: Optional[int] = None,
+                     interleaved: bool = False, sections=None, cyclic: bool = False, factor: float = 1.0, stream=None):
+    """ttf_cache_append: keys (normed and rotated as in ttf_rotate; as they come without positions and freq) and values
+    [rows, heads, channels] of the new tokens into the pages of k_cache and v_cache [pages, page_size, heads, channels] (any
+    strides with contiguous channels).  Rows start[b] .. start[b + 1] - 1 are the last ones of the length[b] tokens of
+    sequence b; slot s lies in page table[b, s // page_size] (all int32 on the device).  With q the queries are normed and
+    rotated by the same kernel; returns out_q (None without q).  Does not synchronise."""
+    if not k.is_cuda:
+        raise ValueError(f"k must be a CUDA tensor, got one on {k.device}")
+    there = _elsewhere(k)
+    if there is not None:
+        with there:
+            return ttf_cache_append(k, v, k_cache, v_cache, start, length, table, positions, freq, q=q, out_q=out_q,
+                                    q_weight=q_weight, k_weight=k_weight, eps=eps, rot_dim=rot_dim, interleaved=interleaved,
+                                    sections=sections, cyclic=cyclic, factor=factor, stream=stream)
+    kh, vh, qh, oq = _heads("k", k, k), _heads("v", v, k), _heads("q", q, k), _NO_HEADS
+    if q is not None:
+        out_q, oq = _out_heads("out_q", out_q, q, k)
+    elif out_q is not None:
+        raise ValueError("out_q without q")
+    if (positions is None) != (freq is None):
+        raise ValueError("positions and freq go together")
+    if positions is not None:
+        pos, rotation = _rotation(positions, freq, q_weight, k_weight, rot_dim, interleaved, sections, cyclic, factor, eps, k)
+    elif q is not None or q_weight is not None or k_weight is not None or rot_dim:
+        raise ValueError("queries and norms need positions and freq")
+    else:
+        pos, rotation = 0, _NO_ROTATION
+    cache, sequences = _cache(k_cache, v_cache, k), _sequences(start, length, table, k)
+    if k.shape[0] == 0:
+        return out_q
+    rc = (_fast or _marshal()).cache_append(*kh, *vh, *qh, pos, 0 if positions is None else 1, *rotation, *sequences, *cache,
+                                            *oq, _stream_of(k, stream))
+    if rc != TTF_OK:
+        raise TTFError(rc, "ttf_cache_append")
+    return out_q
+
+
+def ttf_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, start: torch.Tensor, length: torch.Tensor,
+               table: torch.Tensor, scale: float, *, causal: bool = True, window: int = 0,
+               out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """ttf_attend: attention of the new rows q [rows, heads, channels] over their sequences' slots of the cache, as
+    ttf_cache_append has left it (same start, length and table).  causal: a row sees the slots up to its own; window > 0: of
+    these only the last `window`.  Rows behind start[-1] are left as they are.  Returns out.  Does not synchronise."""
+    if not q.is_cuda:
+        raise ValueError(f"q must be a CUDA tensor, got one on {q.device}")
+    there = _elsewhere(q)
+    if there is not None:
+        with there:
+            return ttf_attend(q, k_cache, v_cache, start, length, table, scale, causal=causal, window=window, out=out,
+                              stream=stream)
+    qh = _heads("q", q, q)
+    out, oh = _out_heads("out", out, q, q)
+    cache, sequences = _cache(k_cache, v_cache, q), _sequences(start, length, table, q)
+    if q.shape[0] == 0:
+        return out
+    rc = (_fast or _marshal()).attend(*qh, *sequences, *cache, scale, 1 if causal else 0, window, *oh, _stream_of(q, stream))
+    if rc != TTF_OK:
+        raise TTFError(rc, "ttf_attend")
+    return out
+
+
+def ttf_paged_status(stream=None) -> int:
+    """ttf_paged_status: synchronises the stream; what ttf_rotate, ttf_cache_append and ttf_attend have reported on the current
+    device since the last query (TTF_OK, TTF_ERR_TIMEOUT or TTF_ERR_BOUNDS)."""
+    v = ctypes.c_int(0)
+    rc = lib().ttf_paged_status(_stream_ptr(stream), ctypes.byref(v))
+    if rc != TTF_OK:
+        raise TTFError(rc, "ttf_paged_status")
+    return int(v.value)
 
 
 def ttf_release() -> None:

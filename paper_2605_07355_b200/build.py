@@ -21,7 +21,7 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-    "-Xcompiler", "-fPIC", "-shared", "-I", INCLUDE,
+    "-Xcompiler", "-fPIC", "-shared", "-I", INCLUDE, "--threads", "0",
 ]
 
 

@@ -8,7 +8,7 @@
 
 #include "ttf.h"
 
-#define NFN 11
+#define NFN 14
 static struct {
     int (*compress)(const void*, int, int, int, int, int, float, int, void*, int*, int*, ttf_stream_t);
     int (*compress_ws)(const void*, int, int, int, int, int, float, int, void*, int*, int*, void*, size_t, ttf_stream_t);
@@ -26,6 +26,11 @@ static struct {
     int (*restore)(const void*, size_t, int, int, int, const int*, const unsigned char*, const int*, void*, int*,
                    ttf_stream_t);
     int (*stats)(const float*, const unsigned char*, const int*, int, int, int, float, float, long long*, ttf_stream_t);
+    int (*rotate)(const ttf_heads*, const ttf_heads*, int, int, int, const int*, const int*, const ttf_rotation*,
+                  const ttf_heads*, const ttf_heads*, ttf_stream_t);
+    int (*cache_append)(const ttf_heads*, const ttf_heads*, const ttf_heads*, const int*, const ttf_rotation*,
+                        const ttf_sequences*, const ttf_cache*, const ttf_heads*, ttf_stream_t);
+    int (*attend)(const ttf_heads*, const ttf_sequences*, const ttf_cache*, float, int, int, const ttf_heads*, ttf_stream_t);
 } fn;
 
 /* the arguments of one call, taken in order; the first conversion that fails leaves a Python error set */
@@ -56,6 +61,13 @@ static size_t size(Args* s) {
     if (!o) return 0;
     size_t v = PyLong_AsSize_t(o);
     if (v == (size_t)-1 && PyErr_Occurred()) s->bad = 1;
+    return v;
+}
+static long long wide(Args* s) {
+    PyObject* o = next_arg(s);
+    if (!o) return 0;
+    long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) s->bad = 1;
     return v;
 }
 static float real(Args* s) {
@@ -101,6 +113,7 @@ static PyObject* m_bind(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     *(void**)&fn.compress_segment = p[3]; *(void**)&fn.compress_batch = p[4]; *(void**)&fn.compress_batch_ex = p[5];
     *(void**)&fn.query = p[6]; *(void**)&fn.query_ws = p[7]; *(void**)&fn.query_ex = p[8];
     *(void**)&fn.restore = p[9]; *(void**)&fn.stats = p[10];
+    *(void**)&fn.rotate = p[11]; *(void**)&fn.cache_append = p[12]; *(void**)&fn.attend = p[13];
     Py_RETURN_NONE;
 }
 
@@ -197,9 +210,73 @@ static PyObject* m_compress_batch(PyObject* self, PyObject* const* a, Py_ssize_t
     return PyLong_FromLong(rc);
 }
 
+/* what the calls over the cache share: heads (address, strides, number), rotation, sequences, cache */
+static ttf_heads heads(Args* s) {
+    ttf_heads h;
+    h.data = ptr(s); h.row_stride = wide(s); h.head_stride = wide(s); h.heads = num(s);
+    return h;
+}
+static const ttf_heads* given(const ttf_heads* h) { return h->data ? h : NULL; }
+static ttf_rotation rotation(Args* s) {
+    ttf_rotation r;
+    r.freq = ptr(s); r.rot_dim = num(s); r.interleaved = num(s); r.axes = num(s);
+    for (int i = 0; i < 3; ++i) r.section[i] = num(s);
+    r.cyclic = num(s); r.factor = real(s); r.q_weight = ptr(s); r.k_weight = ptr(s); r.eps = real(s);
+    return r;
+}
+static ttf_sequences sequences(Args* s) {
+    ttf_sequences q;
+    q.start = ptr(s); q.length = ptr(s); q.table = ptr(s); q.table_stride = wide(s); q.table_pages = num(s); q.seqs = num(s);
+    q.rows = num(s);
+    return q;
+}
+static ttf_cache cache(Args* s) {
+    ttf_cache c;
+    c.k = ptr(s); c.k_page = wide(s); c.k_row = wide(s); c.k_head = wide(s);
+    c.v = ptr(s); c.v_page = wide(s); c.v_row = wide(s); c.v_head = wide(s);
+    c.pages = num(s); c.page_size = num(s); c.heads = num(s); c.head_dim = num(s); c.dtype = num(s);
+    return c;
+}
+/* q, k, head dim, dtype, rows, count, positions, rotation, out_q, out_k, stream */
+static PyObject* m_rotate(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    Args s = {a, n, 0, 0};
+    ttf_heads q = heads(&s), k = heads(&s);
+    int dim = num(&s), dtype = num(&s), rows = num(&s);
+    const int* cnt = ptr(&s); const int* pos = ptr(&s);
+    ttf_rotation r = rotation(&s);
+    ttf_heads oq = heads(&s), ok = heads(&s);
+    ttf_stream_t st = ptr(&s);
+    CALL(fn.rotate(given(&q), given(&k), dim, dtype, rows, cnt, pos, &r, given(&oq), given(&ok), st));
+}
+/* k, v, q, positions, rotated (0: as they come), rotation, sequences, cache, out_q, stream */
+static PyObject* m_cache_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    Args s = {a, n, 0, 0};
+    ttf_heads k = heads(&s), v = heads(&s), q = heads(&s);
+    const int* pos = ptr(&s);
+    int rotated = num(&s);
+    ttf_rotation r = rotation(&s);
+    ttf_sequences sq = sequences(&s);
+    ttf_cache c = cache(&s);
+    ttf_heads oq = heads(&s);
+    ttf_stream_t st = ptr(&s);
+    CALL(fn.cache_append(given(&k), given(&v), given(&q), pos, rotated ? &r : NULL, &sq, &c, given(&oq), st));
+}
+/* q, sequences, cache, scale, causal, window, out, stream */
+static PyObject* m_attend(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    Args s = {a, n, 0, 0};
+    ttf_heads q = heads(&s);
+    ttf_sequences sq = sequences(&s);
+    ttf_cache c = cache(&s);
+    float scale = real(&s); int causal = num(&s), window = num(&s);
+    ttf_heads o = heads(&s);
+    ttf_stream_t st = ptr(&s);
+    CALL(fn.attend(given(&q), &sq, &c, scale, causal, window, given(&o), st));
+}
+
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))m_##name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(bind), METHOD(compress), METHOD(compress_ws), METHOD(compress_segment),
                                 METHOD(compress_batch), METHOD(query), METHOD(query_ws), METHOD(restore), METHOD(stats),
+                                METHOD(rotate), METHOD(cache_append), METHOD(attend),
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__marshal(void) { return PyModule_Create(&module); }

@@ -17,7 +17,7 @@ namespace ttf {
 
 static thread_local int tl_cuda_error = 0;
 
-static int cuda_fail(cudaError_t e) {
+int cuda_fail(cudaError_t e) {
     tl_cuda_error = (int)e;
     return TTF_ERR_CUDA;
 }
@@ -264,6 +264,7 @@ static int clear_control_blocks(void* ws, size_t stride, int n, cudaStream_t st)
 // Checked build: the slack by which every index limit of the next calls is lowered (test hook, normally zero).
 #ifdef TTF_DEBUG
 static std::atomic<int> g_check_slack{0};
+int check_slack() { return g_check_slack.load(); }
 __global__ void k_set_word(int* word, int value, size_t stride) {
     *reinterpret_cast<int*>(reinterpret_cast<uintptr_t>(word) + blockIdx.x * stride) = value;
 }

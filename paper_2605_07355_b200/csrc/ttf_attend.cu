@@ -1,0 +1,8 @@
+// Which kernel attends.
+#include "ttf_paged.cuh"
+
+namespace ttf {
+
+cudaError_t launch_attend(const AttendArgs& a, int dtype, cudaStream_t st) { return launch_attend_simple(a, dtype, st); }
+
+}  // namespace ttf

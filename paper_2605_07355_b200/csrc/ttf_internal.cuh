@@ -177,6 +177,9 @@ cudaError_t launch_stats(const float* sim, const unsigned char* keep, const int*
 // Optional mean fusion (ttf_fuse.cu; not the paper's method): overwrites the anchor block of out_tokens.
 cudaError_t launch_fuse_mean(const Problem& p, const Scratch& s, void* out_tokens, cudaStream_t st);
 
+int cuda_fail(cudaError_t e);      // remembers e for ttf_last_cuda_error; TTF_ERR_CUDA
+int check_slack();                 // checked build: what ttf_debug_set_check_slack has asked for
+
 int sm_count();   // SMs of the current device (cached per device)
 
 // cudaFuncAttributeMaxDynamicSharedMemorySize belongs to a function in the context of ONE device: set it the first
@@ -307,7 +310,8 @@ __device__ __forceinline__ void clear_words(int* hdr, bool fresh) {
 // index outside [0, limit) raises the status word of the call's scratch to 2, leaves (site, index, limit) of the first
 // offender in the header, and the caller skips the access: nothing traps, the context stays usable, and the host
 // reads TTF_ERR_BOUNDS.  In the normal build the test is the constant true and disappears.
-// Sites: 1 sweep, 2 warp-level / CUDA-core matching, 3 tcgen05 matching, 4 gather rows, 5 gather positions.
+// Sites: 1 sweep, 2 warp-level / CUDA-core matching, 3 tcgen05 matching, 4 gather rows, 5 gather positions, 6 rotated heads,
+// 7 cache rows, 8 rows of the attention.
 #ifdef TTF_DEBUG
 __device__ __forceinline__ bool in_bounds(int* hdr, int site, long long idx, long long limit) {
     limit -= __ldcg(hdr + HDR_CHECK_SLACK);
