@@ -1,0 +1,565 @@
+// Attention of new rows over a paged cache on the fifth-generation tensor cores: bf16, heads of up to 128 channels.
+//
+//   S = Q K^T,  t = scale log2(e) S,  P = exp2(t - m),  O += P V,  l += sum P,  o = O / l
+//
+// The new tokens of a sequence times the query heads of a group are the rows of a tile (row = token * group + head), so that a
+// group reads its keys and values once.  A CTA takes two tiles of up to 128 rows of one sequence and key head and walks their
+// slots in blocks of (up to) 128:
+//   warp 8       TMA: the pages of a block, keys then values, into a ring of [128 slots x DP channels] slots (128-byte swizzle;
+//                channels beyond the head arrive as zeros)
+//   warp 9       tcgen05.mma: S0 = Q0 K^T, S1 = Q1 K^T (both operands in shared memory), O0 += P0 V, O1 += P1 V (P in tensor
+//                memory, V read as the transposed operand)
+//   warps 0 - 3  softmax of tile 0, one row per thread; warps 4 - 7 the same for tile 1
+// While one tile's weights are formed the other tile's products run: O0 += P0 V(j), S0 = Q0 K(j+1)^T, O1 += P1 V(j),
+// S1 = Q1 K(j+1)^T.  P takes the place of its scores in tensor memory, so the next scores of a tile are only asked for when the
+// product before has completed; when scores arrive nobody touches O, and the softmax threads rescale it themselves.  They do so
+// only where a maximum has grown by more than 8 (in powers of two: weights stay below 2^8, l and O carry the same factor, and
+// nothing is lost, since bf16 and fp32 keep their relative precision), which after the first blocks is rare.
+//
+// Few tiles over many slots: the CTAs of a cluster share the blocks, and each finishes a part of the rows from what all of them
+// leave in shared memory.
+//
+// Masks: only blocks that some row of the tile does not see whole are masked, by selection, whatever the keys hold.  Values of
+// slots that no row of the CTA sees (stale rows of a page behind the length, slots before the window) are zeroed in shared memory.
+//
+// Every mbarrier wait is bounded; a wait that runs out is reported, the CTA's roles stop, wait (bounded) for their copies and
+// products in flight, free the tensor memory and return.
+#include <cuda.h>
+
+#include "ttf_paged.cuh"
+#include "ttf_async.cuh"
+#include "ttf_cluster.cuh"
+#include "ttf_tcgen05.cuh"
+#include "ttf_tensormap.cuh"
+
+namespace ttf {
+
+constexpr int kAtRows = 128;                       // rows of a tile = tensor-memory lanes
+constexpr int kAtSlots = 128;                      // slots of a block
+constexpr int kAtThreads = 320;
+
+template <int DP> struct AttendShape {
+    static constexpr int HALVES = DP / 64;                         // 128-byte columns of a row
+    static constexpr int COL = 128 * 128;                          // bytes of one such column of 128 rows
+    static constexpr int TILE = HALVES * COL;                      // a Q tile, a ring slot
+    static constexpr int RING = DP == 128 ? 5 : 8;
+    static constexpr int SMEM = 2 * TILE + RING * TILE;
+    static constexpr int OP = DP + 4;                              // floats of a row that ranks exchange; behind both tiles'
+    static constexpr int ML = 2 * kAtRows * OP;                    // rows [maximum, sum][tile][row]
+    static constexpr uint32_t O_COL = 256;                         // tensor memory: S0 0, S1 128, O0, O1 from 256 on
+};
+
+struct AttendMaps { CUtensorMap q, k, v; };
+
+// D[tmem] (+)= A[tmem] . B[smem desc], issued by one thread
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"((uint32_t)accumulate)
+        : "memory");
+}
+// operand whose rows (128 bytes: 64 elements along N, swizzled) run along K: 8-row groups 1024 bytes apart, the next 64
+// elements of N `lead` bytes further
+__device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t smem_addr, uint32_t lead) {
+    return (smem_desc_sw128(smem_addr) & ~((uint64_t)0x3FFF << 16)) | ((uint64_t)(lead >> 4) << 16);
+}
+// bf16 x bf16 -> fp32, M = 128; b_mn: B runs along N
+__host__ __device__ constexpr uint32_t idesc_attend(int n, bool b_mn) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
+}
+
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int c0, int c1, int c2, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(bar))
+        : "memory");
+}
+
+// 32 consecutive columns of this thread's tensor-memory lane
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+          "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+          "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
+          "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
+          "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+// the loads above have completed; the registers are operands of something behind the wait, so that nothing that reads them
+// can be moved before it
+template <int N> __device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[N]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < N; i += 8)
+        asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]),
+                          "+r"(r[i + 6]), "+r"(r[i + 7]) :: "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float ld_cluster_f32_(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+template <int DP>
+__global__ void __launch_bounds__(kAtThreads, 1)
+k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ AttendArgs a, int lsplit, int per_tile, int block,
+            int box_rows)
+{
+    using S = AttendShape<DP>;
+    extern __shared__ unsigned char at_raw[];
+    __shared__ uint64_t bar_q, bar_full[S::RING], bar_empty[S::RING], bar_s[2], bar_p[2], bar_pv[2], bar_end;
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_err;
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int split = 1 << lsplit, rank = lsplit ? (int)cluster_rank() : 0;
+    const int work = blockIdx.x >> lsplit;
+    const int hk = work % a.cache.heads;
+    const int limit = a.wait_limit;
+
+    pdl_wait();
+    Tile t;
+    // (every CTA of a cluster has the same tile, and so the same answer)
+    if (!find_tile(a, 0, 2 * per_tile, work / a.cache.heads, blockIdx.x == 0, t)) return;
+    const SeqRange r = t.r;
+    const int tok0 = t.tile * 2 * per_tile;                // first token of the CTA
+    int ntok[2];
+    ntok[0] = min(per_tile, r.n - tok0);
+    ntok[1] = max(0, min(per_tile, r.n - tok0 - per_tile));
+
+    // the blocks of this rank, and of each of its tiles
+    const int tok_z = tok0 + ntok[0] + ntok[1] - 1;
+    const int lo_u = seen_by(r, tok0, a.causal, a.window).lo, hi_u = seen_by(r, tok_z, a.causal, a.window).hi;
+    const int b_lo = lo_u / block, b_hi = hi_u > lo_u ? (hi_u + block - 1) / block : b_lo;
+    const int j_lo = b_lo + (int)((long long)(b_hi - b_lo) * rank >> lsplit);
+    const int j_hi = b_lo + (int)((long long)(b_hi - b_lo) * (rank + 1) >> lsplit);
+    int jt_lo[2], jt_hi[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const int ta = tok0 + x * per_tile;
+        const int lo = seen_by(r, ta, a.causal, a.window).lo, hi = seen_by(r, ta + ntok[x] - 1, a.causal, a.window).hi;
+        jt_lo[x] = max(j_lo, lo / block);
+        jt_hi[x] = ntok[x] > 0 && hi > lo ? min(j_hi, (hi + block - 1) / block) : 0;
+        if (jt_hi[x] < jt_lo[x]) jt_hi[x] = jt_lo[x];
+    }
+
+    const uint32_t base_addr = (smem_u32(at_raw) + 1023u) & ~1023u;
+    unsigned char* const smem = at_raw + (base_addr - smem_u32(at_raw));
+    if (tid == 0) {
+        mbar_init(&bar_q, 1);
+        mbar_init(&bar_end, 1);
+        for (int s = 0; s < S::RING; ++s) { mbar_init(&bar_full[s], 1); mbar_init(&bar_empty[s], 1); }
+        for (int x = 0; x < 2; ++x) { mbar_init(&bar_s[x], 1); mbar_init(&bar_p[x], 4); mbar_init(&bar_pv[x], 1); }
+        mbar_init_fence();
+        s_err = 0;
+        tensormap_prefetch(&maps.q); tensormap_prefetch(&maps.k); tensormap_prefetch(&maps.v);
+    }
+    // rows of the ring that no page fills (blocks of less than 128 slots): zero for good
+    if (block < kAtSlots) {
+        const int n = (kAtSlots - block) * 8;              // 16-byte pieces of a column
+        for (int i = tid; i < n * S::RING * S::HALVES; i += kAtThreads) {
+            const int col = i / n, o = i - col * n;
+            *reinterpret_cast<uint4*>(smem + 2 * S::TILE + (size_t)col * S::COL + block * 128 + o * 16) = make_uint4(0, 0, 0, 0);
+        }
+        fence_async_smem();
+    }
+    if (warp == 9) tmem_alloc(&s_tmem, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    auto failed = [&]() { return *(volatile int*)&s_err != 0; };
+    auto give_up = [&]() { atomicExch(&s_err, 1); };
+
+    if (warp == 8) {
+        // ---- producer -------------------------------------------------------------------------------------------
+        bool bad = false;
+        if (lane == 0 && j_lo < j_hi) {
+            const int tiles = ntok[1] > 0 ? 2 : 1;
+            mbar_arrive_expect_tx(&bar_q, (uint32_t)(tiles * S::HALVES * per_tile * a.group * 128 + a.tx_extra));
+            for (int x = 0; x < tiles; ++x)
+                for (int h = 0; h < S::HALVES; ++h)
+                    tma_load_3d(smem + x * S::TILE + h * S::COL, &maps.q, h * 64, hk * a.group, r.first + tok0 + x * per_tile, &bar_q);
+        }
+        const int* const table = a.seq.table + (long long)t.seq * a.seq.table_stride;
+        const int page = (int)a.cache.page.d;
+        int issued = 0;
+        auto page_id = [&](int j) {                        // lane = page of the block (box_rows rows each)
+            const int s0 = j * block + lane * box_rows;
+            if (lane * box_rows >= block || j >= j_hi || s0 >= hi_u || s0 + box_rows <= lo_u) return -1;
+            return page_of(table, quotient(s0, a.cache.page), a.cache.pages, bad);
+        };
+        int id = page_id(j_lo);
+        for (int j = j_lo; j < j_hi; ++j) {
+            const int next = page_id(j + 1);
+            const uint32_t bytes = (uint32_t)(__popc(__ballot_sync(0xffffffffu, id >= 0)) * box_rows * 128 * S::HALVES);
+            const int row = j * block + lane * box_rows - quotient(j * block + lane * box_rows, a.cache.page) * page;
+            bool ok = true;
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                const int idx = 2 * (j - j_lo) + kv, slot = idx % S::RING;
+                if (idx >= S::RING && !mbar_wait(&bar_empty[slot], ((idx / S::RING) & 1) ^ 1, limit)) { give_up(); ok = false; }
+                ok = __all_sync(0xffffffffu, ok && !failed());
+                if (!ok) break;
+                if (lane == 0) mbar_arrive_expect_tx(&bar_full[slot], bytes + (uint32_t)a.tx_extra);
+                __syncwarp();
+                if (id >= 0) {
+                    unsigned char* dst = smem + 2 * S::TILE + slot * S::TILE + lane * box_rows * 128;
+                    const CUtensorMap* map = kv ? &maps.v : &maps.k;
+#pragma unroll
+                    for (int h = 0; h < S::HALVES; ++h) tma_load_4d(dst + h * S::COL, map, h * 64, row, hk, id, &bar_full[slot]);
+                }
+                issued = idx + 1;
+            }
+            if (!ok) break;
+            id = next;
+        }
+        if (__any_sync(0xffffffffu, bad) && lane == 0) report_paged(a.hdr, 2);
+        if (failed()) {                                    // copies in flight land before the CTA may leave
+            if (j_lo < j_hi) mbar_wait(&bar_q, 0, limit);
+            for (int i = issued > S::RING ? issued - S::RING : 0; i < issued; ++i)
+                mbar_wait(&bar_full[i % S::RING], (i / S::RING) & 1, limit);
+        }
+    } else if (warp == 9) {
+        // ---- products ---------------------------------------------------------------------------------------------
+        constexpr uint32_t id_s = idesc_attend(kAtSlots, false), id_o = idesc_attend(DP, true);
+        bool ok = true;
+        auto wait = [&](uint64_t* bar, int parity) {
+            if (ok && !__all_sync(0xffffffffu, !failed() && mbar_wait(bar, parity, limit))) { ok = false; give_up(); }
+        };
+        auto ring = [&](int idx) { return base_addr + 2 * S::TILE + (uint32_t)(idx % S::RING) * S::TILE; };
+        auto scores = [&](int x, int j) {                  // S_x = Q_x K(j)^T
+            if (lane == 0) {
+                const uint64_t dq = smem_desc_sw128(base_addr + x * S::TILE), dk = smem_desc_sw128(ring(2 * (j - j_lo)));
+#pragma unroll
+                for (int k = 0; k < DP / 16; ++k) {
+                    const uint64_t at = (uint64_t)(((k / 4) * S::COL + (k % 4) * 32) >> 4);
+                    umma_bf16(tmem + x * 128, dq + at, dk + at, id_s, k > 0);
+                }
+                umma_commit(&bar_s[x]);
+            }
+            __syncwarp();
+        };
+        auto weigh = [&](int x, int j) {                   // O_x += P_x V(j)
+            if (lane == 0) {
+                const uint64_t dv = smem_desc_sw128_mn(ring(2 * (j - j_lo) + 1), S::COL);
+#pragma unroll
+                for (int k = 0; k < kAtSlots / 16; ++k)
+                    umma_bf16_ts(tmem + S::O_COL + x * DP, tmem + x * 128 + k * 8, dv + (uint64_t)(k * (16 * 128 >> 4)), id_o,
+                                 k > 0 || j > jt_lo[x]);
+                umma_commit(&bar_pv[x]);
+            }
+            __syncwarp();
+        };
+        auto done_with = [&](int idx) { if (lane == 0) umma_commit(&bar_empty[idx % S::RING]); __syncwarp(); };
+        auto has = [&](int x, int j) { return j >= jt_lo[x] && j < jt_hi[x]; };
+        if (j_lo < j_hi) {
+            wait(&bar_q, 0);
+            wait(&bar_full[0], 0);
+            tc_fence_after();
+            if (ok) {
+                for (int x = 0; x < 2; ++x) if (has(x, j_lo)) scores(x, j_lo);
+                done_with(0);
+            }
+        }
+        for (int j = j_lo; j < j_hi && ok; ++j) {
+            const int iv = 2 * (j - j_lo) + 1, ik = iv + 1;
+            wait(&bar_full[iv % S::RING], (iv / S::RING) & 1);
+            // values of slots that no row of the CTA sees
+            const int s0 = j * block;
+            if (ok && (s0 < lo_u || s0 + block > hi_u)) {
+                const int head = max(0, lo_u - s0), tail = min(block, hi_u - s0);
+                unsigned char* v = smem + (ring(iv) - base_addr);
+                for (int i = lane; i < block * 8 * S::HALVES; i += 32) {
+                    const int h = i / (block * 8), o = i - h * (block * 8), row = o >> 3;
+                    if (row < head || row >= tail) *reinterpret_cast<uint4*>(v + h * S::COL + o * 16) = make_uint4(0, 0, 0, 0);
+                }
+                fence_async_smem();
+                __syncwarp();
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                if (has(x, j)) {
+                    wait(&bar_p[x], (j - jt_lo[x]) & 1);
+                    tc_fence_after();
+                    if (ok) weigh(x, j);
+                }
+                if (x == 1) done_with(iv);
+                if (j + 1 < j_hi) {
+                    if (x == 0) wait(&bar_full[ik % S::RING], (ik / S::RING) & 1);
+                    if (has(x, j)) wait(&bar_pv[x], (j - jt_lo[x]) & 1);
+                    tc_fence_after();
+                    if (has(x, j + 1) && ok) scores(x, j + 1);
+                    if (x == 1) done_with(ik);
+                }
+            }
+        }
+    } else {
+        // ---- softmax: one row per thread ----------------------------------------------------------------------------
+        const int x = warp >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t s_at = lanes + x * 128, o_at = lanes + S::O_COL + x * DP;
+        const int nrow = ntok[x] * a.group;
+        const Seen mine = row < nrow ? seen_by(r, tok0 + x * per_tile + row / a.group, a.causal, a.window) : Seen{0, 0};
+        // slots that every row of the tile sees
+        const int all_lo = ntok[x] > 0 ? seen_by(r, tok0 + x * per_tile + ntok[x] - 1, a.causal, a.window).lo : 0;
+        const int all_hi = ntok[x] > 0 ? seen_by(r, tok0 + x * per_tile, a.causal, a.window).hi : 0;
+        const float c = a.scale * 1.4426950408889634f;
+        float m = -INFINITY, l = 0.f;
+        bool ok = true;
+        for (int j = jt_lo[x]; j < jt_hi[x]; ++j) {
+            const int n = j - jt_lo[x];
+            if (!__all_sync(0xffffffffu, !failed() && mbar_wait(&bar_s[x], n & 1, limit))) { give_up(); ok = false; break; }
+            tc_fence_after();
+            uint32_t s[128];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tmem_ld32(s_at + i * 32, s + i * 32);
+            tmem_ld_wait(s);
+            const int s0 = j * block;
+            if (block < kAtSlots || s0 < all_lo || s0 + kAtSlots > all_hi) {
+                const int lo = mine.lo - s0, hi = min(mine.hi - s0, block);
+#pragma unroll
+                for (int i = 0; i < 128; ++i) s[i] = i >= lo && i < hi ? s[i] : 0xff800000u;
+            }
+            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int i = 0; i < 128; i += 8)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    mx[e] = fmaxf(mx[e], fmaxf(__uint_as_float(s[i + e]), __uint_as_float(s[i + 4 + e])));
+            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+            const bool grown = top > m + 8.f;              // (m = -inf: any number is)
+            if (__any_sync(0xffffffffu, grown)) {
+                const float m1 = grown ? top : m;
+                const float f = m == m1 ? 1.f : exp2_approx(m - m1);
+                m = m1;
+                l *= f;
+                if (n > 0) {
+#pragma unroll 1
+                    for (int i = 0; i < DP; i += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(o_at + i, o);
+                        tmem_ld_wait(o);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                        tmem_st32(o_at + i, o);
+                    }
+                }
+            }
+            const float ref = m == -INFINITY ? 0.f : m;
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t p[32];
+#pragma unroll
+                for (int i = 0; i < 64; i += 2) {
+                    const float p0 = exp2_approx(fmaf(__uint_as_float(s[h * 64 + i]), c, -ref));
+                    const float p1 = exp2_approx(fmaf(__uint_as_float(s[h * 64 + i + 1]), c, -ref));
+                    sum[(i & 2)] += p0; sum[(i & 2) + 1] += p1;
+                    p[i / 2] = bf16_pair(p0, p1);
+                }
+                tmem_st32(s_at + h * 32, p);
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar_p[x]);
+        }
+        const int n = jt_hi[x] - jt_lo[x];
+        if (n > 0 && ok && !mbar_wait(&bar_pv[x], (n - 1) & 1, limit)) give_up();
+        __syncwarp();
+        tc_fence_after();
+        if (lsplit == 0) {
+            if (row < nrow || n > 0) {                     // (whole warps take part in the loads from tensor memory)
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                const int token = tok0 + x * per_tile + (row < nrow ? row / a.group : 0);
+                const int head = hk * a.group + (row < nrow ? row % a.group : 0);
+                uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<bf16_t*>(a.out.data) + (long long)(r.first + token) * a.out.row + (long long)head * a.out.head);
+                const bool on = row < nrow && in_bounds(a.hdr, 8, (long long)r.first + token, a.seq.rows);
+#pragma unroll 1
+                for (int i = 0; i < DP; i += 32) {
+                    uint32_t o[32];
+                    if (n > 0) { tmem_ld32(o_at + i, o); tmem_ld_wait(o); }
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        uint4 w = make_uint4(0, 0, 0, 0);
+                        if (n > 0 && l != 0.f) {
+                            w.x = bf16_pair(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
+                            w.y = bf16_pair(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
+                            w.z = bf16_pair(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
+                            w.w = bf16_pair(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
+                        }
+                        if (on && i + e < a.cache.dim) dst[(i + e) / 8] = w;
+                    }
+                }
+            }
+        } else {
+            // the other tile's products may still read the ring: what is exchanged goes where Q and the ring were, so both
+            // tiles have to be through
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            float* const ml = reinterpret_cast<float*>(smem) + S::ML + x * kAtRows + row;
+            ml[0] = m; ml[2 * kAtRows] = l;
+            float* const mine_o = reinterpret_cast<float*>(smem) + (x * kAtRows + row) * S::OP;
+            if (n > 0) {
+#pragma unroll 1
+                for (int i = 0; i < DP; i += 32) {
+                    uint32_t o[32];
+                    tmem_ld32(o_at + i, o);
+                    tmem_ld_wait(o);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        *reinterpret_cast<float4*>(mine_o + i + e) = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]),
+                                                                                  __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
+                }
+            }
+        }
+    }
+    pdl_launch_dependents();
+
+    if (lsplit) {
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+        // rows row % split == rank of both tiles, four channels per thread
+        constexpr int Q4 = DP / 4;
+        for (int e = tid; e < 2 * (kAtRows >> lsplit) * Q4; e += kAtThreads) {
+            const int d = (e % Q4) * 4, x = (e / Q4) & 1, row = ((e / Q4) >> 1 << lsplit) + rank;
+            if (row >= ntok[x] * a.group || d >= a.cache.dim) continue;
+            const uint32_t at_m = base_addr + (uint32_t)(S::ML + x * kAtRows + row) * 4, at_l = at_m + 2 * kAtRows * 4;
+            const uint32_t at_o = base_addr + (uint32_t)((x * kAtRows + row) * S::OP + d) * 4;
+            float m = -INFINITY;
+            for (int p = 0; p < split; ++p) m = fmaxf(m, ld_cluster_f32_(cluster_addr(at_m, p)));
+            const float ref = m == -INFINITY ? 0.f : m;
+            float l = 0.f;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int p = 0; p < split; ++p) {
+                const float lp = ld_cluster_f32_(cluster_addr(at_l, p));
+                if (lp == 0.f) continue;                   // that rank saw nothing of the row
+                const float f = exp2_approx(ld_cluster_f32_(cluster_addr(at_m, p)) - ref);
+                const float4 v = ld_cluster_f32x4(cluster_addr(at_o, p));
+                l = fmaf(f, lp, l);
+                o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+            }
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const int token = tok0 + x * per_tile + row / a.group, head = hk * a.group + row % a.group;
+            uint2 w = make_uint2(0, 0);
+            if (l != 0.f) w = make_uint2(bf16_pair(o.x * inv, o.y * inv), bf16_pair(o.z * inv, o.w * inv));
+            if (in_bounds(a.hdr, 8, (long long)r.first + token, a.seq.rows))
+                *reinterpret_cast<uint2*>(reinterpret_cast<bf16_t*>(a.out.data) + (long long)(r.first + token) * a.out.row + (long long)head * a.out.head + d) = w;
+        }
+        cluster_arrive();                                  // nobody leaves while its sums may be read
+        cluster_wait();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        if (s_err) {                                       // products in flight end before their accumulators are given back
+            if (lane == 0) umma_commit(&bar_end);
+            __syncwarp();
+            mbar_wait(&bar_end, 0, limit);
+        }
+        tmem_dealloc(tmem, 512);
+    }
+    if (tid == 0 && s_err) report_paged(a.hdr, 1);
+}
+
+// ---- host side ------------------------------------------------------------------------------------------------------
+static bool tma_ok(const void* p, long long s0, long long s1, long long s2) {
+    auto fine = [](long long s) { return s >= 0 && s % 8 == 0 && s < (1LL << 38); };
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && fine(s0) && fine(s1) && fine(s2);
+}
+
+bool attend_tc_takes(const AttendArgs& a, int dtype) {
+    const int page = (int)a.cache.page.d;
+    return dtype == TTF_DTYPE_BF16 && a.cache.dim % 8 == 0 && a.cache.dim <= 128 && a.group <= kAtRows && a.scale > 0.f &&
+           page % 8 == 0 && (page <= kAtSlots || page % kAtSlots == 0) &&
+           tma_ok(a.q.data, a.q.row, a.q.head, 0) && tma_ok(a.cache.k, a.cache.k_page, a.cache.k_row, a.cache.k_head) &&
+           tma_ok(a.cache.v, a.cache.v_page, a.cache.v_row, a.cache.v_head) && tma_ok(a.out.data, a.out.row, a.out.head, 0) &&
+           encode_fn() != nullptr;
+}
+
+// a map over axes of `n` elements with strides of `s` elements (0: an axis of one element, whose stride does not matter)
+static bool encode(CUtensorMap* m, const void* data, int rank, const long long* n, const long long* s, const int* box) {
+    cuuint64_t dims[4], strides[3];
+    cuuint32_t bx[4], one[4] = {1, 1, 1, 1};
+    for (int i = 0; i < rank; ++i) { dims[i] = (cuuint64_t)n[i]; bx[i] = (cuuint32_t)box[i]; }
+    for (int i = 1; i < rank; ++i) strides[i - 1] = (cuuint64_t)(s[i] > 0 ? s[i] * 2 : 16);
+    return encode_fn()(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(data), dims, strides, bx, one,
+                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DP> static cudaError_t launch_tc_t(const AttendArgs& a, cudaStream_t st) {
+    using S = AttendShape<DP>;
+    const int page = (int)a.cache.page.d, per = kAtRows / a.group;
+    const int block = page < kAtSlots ? kAtSlots / page * page : kAtSlots, box = page < kAtSlots ? page : kAtSlots;
+    AttendMaps maps;
+    {
+        const long long n[3] = {a.cache.dim, a.q.heads, a.seq.rows}, s[3] = {1, a.q.head, a.q.row};
+        const int b[3] = {64, a.group, per};
+        if (!encode(&maps.q, a.q.data, 3, n, s, b)) return cudaErrorInvalidValue;
+    }
+    for (int kv = 0; kv < 2; ++kv) {
+        const long long n[4] = {a.cache.dim, page, a.cache.heads, a.cache.pages};
+        const long long s[4] = {1, kv ? a.cache.v_row : a.cache.k_row, kv ? a.cache.v_head : a.cache.k_head, kv ? a.cache.v_page : a.cache.k_page};
+        const int b[4] = {64, box, 1, 1};
+        if (!encode(kv ? &maps.v : &maps.k, kv ? a.cache.v : a.cache.k, 4, n, s, b)) return cudaErrorInvalidValue;
+    }
+    const void* fn = reinterpret_cast<const void*>(k_attend_tc<DP>);
+    const size_t smem = S::SMEM + 1024;
+    cudaError_t e = ensure_dynamic_smem(fn, smem);
+    if (e != cudaSuccess) return e;
+    const long long ctas = most_tiles(a, 0, 2 * per) * a.cache.heads;
+    const long long slots = (long long)a.seq.table_pages * page;
+    const long long reach = (long long)a.window + a.seq.rows, longest = a.window > 0 && reach < slots ? reach : slots;
+    int ls = 0;
+    while (ls < 3 && (ctas << (ls + 1)) <= sm_count() && (longest >> (ls + 1)) >= 2 * kAtSlots) ++ls;
+    if ((ctas << ls) > 0x7fffffffLL) return cudaErrorInvalidValue;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(ctas << ls)); cfg.blockDim = dim3(kAtThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 1u << ls; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = ls ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, k_attend_tc<DP>, maps, a, ls, per, block, box);
+}
+cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t st) {
+    return a.cache.dim <= 64 ? launch_tc_t<64>(a, st) : launch_tc_t<128>(a, st);
+}
+
+}  // namespace ttf

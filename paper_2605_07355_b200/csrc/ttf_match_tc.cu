@@ -41,6 +41,7 @@
 #include "ttf_internal.cuh"
 #include "ttf_async.cuh"
 #include "ttf_cluster.cuh"
+#include "ttf_tcgen05.cuh"
 #include "ttf_tensormap.cuh"
 
 #include <atomic>
@@ -54,31 +55,7 @@ constexpr int kTcKC = 64;                // channels per stage (128 bytes: one s
 constexpr int kTcABytes = kTcM * 128;    // 16 KB
 constexpr int kTcThreads = 192;
 
-// ---- PTX wrappers -----------------------------------------------------------------------------------------
-__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// whole warp: allocates `cols` (a power of two >= 32) columns of tensor memory, base address -> *dst_smem
-__device__ __forceinline__ void tmem_alloc(uint32_t* dst_smem, uint32_t cols) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst_smem)), "r"(cols) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t cols) {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
-}
-// D[tmem] (+)= A[smem desc] . B[smem desc]^T, issued by one thread
-__device__ __forceinline__ void umma_bf16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, bool accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"((uint32_t)accumulate)
-        : "memory");
-}
-// the barrier receives one arrival when every MMA issued so far by this thread has completed
-__device__ __forceinline__ void umma_commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
+// ---- tensor memory of the epilogue -------------------------------------------------------------------------
 // 8 NG consecutive fp32 columns of this thread's tensor-memory lane
 template <int NG> __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[NG][8]) {
 #pragma unroll
@@ -103,16 +80,6 @@ template <int NG> __device__ __forceinline__ void tmem_add(uint32_t (&a)[NG][8],
 }
 __device__ __forceinline__ void epilogue_bar_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
-// K-major operand tile with the 128-byte swizzle: rows of 128 bytes, groups of 8 rows 1024 bytes apart
-__device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t smem_addr) {
-    uint64_t d = 0;
-    d |= (uint64_t)((smem_addr & 0x3FFFF) >> 4);          // start address, 16-byte units
-    d |= (uint64_t)1 << 16;                               // leading byte offset (not used by swizzled K-major)
-    d |= (uint64_t)(1024 >> 4) << 32;                     // stride byte offset between 8-row groups
-    d |= (uint64_t)1 << 46;                               // descriptor version of sm_100
-    d |= (uint64_t)2 << 61;                               // 128-byte swizzle
-    return d;
-}
 // bf16 x bf16 -> fp32, A and B K-major, M = 128, N = NB
 __host__ __device__ constexpr uint32_t idesc_bf16(int NB) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NB >> 3) << 17) | ((uint32_t)(kTcM >> 4) << 24);
@@ -493,11 +460,7 @@ k_match_tc(const __grid_constant__ ClipMaps<G> maps, int F, int H, int W, int C,
 }
 
 // ---- host side: tensor maps and launch ------------------------------------------------------------------------
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeTiledFn encode_fn() {
+EncodeTiledFn encode_fn() {
     static std::mutex mu;
     static EncodeTiledFn fn = nullptr;
     std::lock_guard<std::mutex> lk(mu);

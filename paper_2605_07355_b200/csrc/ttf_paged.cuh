@@ -70,6 +70,8 @@ struct AttendArgs {
     int* hdr;
 };
 cudaError_t launch_attend(const AttendArgs& a, int dtype, cudaStream_t st);
+bool attend_tc_takes(const AttendArgs& a, int dtype);
+cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t st);
 cudaError_t launch_attend_simple(const AttendArgs& a, int dtype, cudaStream_t st);
 
 // Upper bound on the tiles of a call (the host does not know how the rows are spread over the sequences), and the CTAs of a
@@ -141,7 +143,7 @@ __device__ __forceinline__ SeqRange seq_range(const SeqView& s, int b, const Div
     r.first = __ldcg(s.start + b);
     const int end = __ldcg(s.start + b + 1);
     r.length = __ldcg(s.length + b);
-    r.ok = r.first >= 0 && end >= r.first && end <= s.rows && r.length >= 0 &&
+    r.ok = r.first >= 0 && end >= r.first && end <= s.rows && r.length >= 0 && r.length <= (1 << 30) &&
            (long long)r.length <= (long long)s.table_pages * page.d;
     r.n = r.ok ? end - r.first : 0;
     return r;

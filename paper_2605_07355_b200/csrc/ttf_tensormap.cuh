@@ -12,6 +12,11 @@ namespace ttf {
 // launch over one clip has a type of its own: 256 bytes instead of 4 KB to hand over with every launch.
 template <int G> struct ClipMaps { CUtensorMap a[G], b[G]; };
 
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_fn();         // the driver's cuTensorMapEncodeTiled; NULL where it is not to be had
+
 // Tile of (kc channels, bw cells, bh rows, bf frames) elements, zeros outside X; swizzle128: the 128-byte swizzle
 // (kc * element size must be 128 bytes), else rows of the tile are stored plainly.  dtype 0 fp32, 1 bf16.
 bool make_tensor_map(CUtensorMap* m, const void* X, int dtype, int F, int H, int W, int C, int kc, int bw, int bh, int bf,
