@@ -52,7 +52,7 @@ struct RotateArgs {
     const int* pos;
     const float* freq;                             // NULL: no rotation and no norm (append of keys as they come)
     int rot, interleaved, axes, sec1, sec2, sec0, cyclic;
-    float factor, eps;
+    float factor, eps, inv_dim;
     const void *q_weight, *k_weight;
     SeqView seq;                                   // append only
     CacheView cache;
@@ -95,13 +95,6 @@ template <> struct VecIO<float, 1> { using Raw = uint32_t; };
 __device__ __forceinline__ uint16_t load_cg(const uint16_t* p) { return __ldcg(reinterpret_cast<const unsigned short*>(p)); }
 template <typename R> __device__ __forceinline__ R load_cg(const R* p) { return __ldcg(p); }
 
-// fp32 -> bf16, round to nearest even (NaN stays NaN)
-__device__ __forceinline__ uint32_t to_bf16(float x) {
-    uint32_t r;
-    asm("{.reg .b16 h; cvt.rn.bf16.f32 h, %1; mov.b32 %0, {h, h};}" : "=r"(r) : "f"(x));
-    return r & 0xffffu;
-}
-
 template <int V> __device__ __forceinline__ void unpack(const typename VecIO<bf16_t, V>::Raw& r, float (&x)[V], bf16_t) {
     if constexpr (V == 1) x[0] = __uint_as_float((uint32_t)r << 16);
     else {
@@ -115,13 +108,19 @@ template <int V> __device__ __forceinline__ void unpack(const typename VecIO<flo
 #pragma unroll
     for (int i = 0; i < V; ++i) x[i] = __uint_as_float(w[i]);
 }
+// two fp32 -> bf16, round to nearest even (NaN stays NaN)
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
 template <int V> __device__ __forceinline__ typename VecIO<bf16_t, V>::Raw pack(const float (&x)[V], bf16_t) {
     typename VecIO<bf16_t, V>::Raw r;
-    if constexpr (V == 1) r = (uint16_t)to_bf16(x[0]);
+    if constexpr (V == 1) r = (uint16_t)(bf16_pair(x[0], x[0]) & 0xffffu);
     else {
         uint32_t* w = reinterpret_cast<uint32_t*>(&r);
 #pragma unroll
-        for (int i = 0; i < V / 2; ++i) w[i] = to_bf16(x[2 * i]) | (to_bf16(x[2 * i + 1]) << 16);
+        for (int i = 0; i < V / 2; ++i) w[i] = bf16_pair(x[2 * i], x[2 * i + 1]);
     }
     return r;
 }

@@ -130,7 +130,7 @@ int ttf_rotate(const ttf_heads* q, const ttf_heads* k, int head_dim, int dtype, 
     RotateArgs a = {};
     TTF_CHECK(paged_words(&a.hdr));
     a.q = ttf::view(q, rows); a.k = ttf::view(k, rows); a.out_q = ttf::view(out_q, rows); a.out_k = ttf::view(out_k, rows);
-    a.dim = head_dim; a.rows = rows; a.count = count;
+    a.dim = head_dim; a.inv_dim = 1.f / head_dim; a.rows = rows; a.count = count;
     take_rotation(rotation, positions, &a);
     a.cache.page = make_divisor(1);
     Range range("ttf rotate");
@@ -153,7 +153,7 @@ int ttf_cache_append(const ttf_heads* k, const ttf_heads* v, const ttf_heads* q,
     TTF_CHECK(paged_words(&a.hdr));
     const int rows = sequences->rows;
     a.q = ttf::view(q, rows); a.k = ttf::view(k, rows); a.v = ttf::view(v, rows); a.out_q = ttf::view(out_q, rows);
-    a.dim = cache->head_dim; a.rows = sequences->rows;
+    a.dim = cache->head_dim; a.inv_dim = 1.f / cache->head_dim; a.rows = sequences->rows;
     take_rotation(rotation, positions, &a);
     a.seq = ttf::view(sequences); a.cache = ttf::view(cache);
     Range range("ttf cache append");

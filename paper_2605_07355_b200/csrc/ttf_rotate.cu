@@ -4,17 +4,25 @@
 //   y = x * w / sqrt(mean(x^2) + eps);   (u, v) -> factor * (u cos a - v sin a, v cos a + u sin a),   a = p[axis(j)] * freq[j]
 //
 // Bound by memory: every head is read once, kept in registers between the sum of squares and the rotation, and written
-// once.  All heads of a row turn by the same angles, so a CTA takes whole rows: its first rot / 2 threads form the row's
-// cosines and sines in shared memory (in turns, in 64 bits: an fp32 product loses the turn from positions of about 10^4
-// on) while the heads' loads are in flight.  A head is an item of two V-channel vectors per lane (for the half layout the
-// two halves of V pairs), the lanes of a head are the power of two that covers it, and a warp holds 32 / lanes heads.
-// CTAs walk the rows with a stride, so that the worst-case capacity behind a count that only the device knows costs nothing;
-// where there are fewer rows than places the heads of a row are spread over several CTAs.
+// once.  All heads of a row turn by the same angles, so a warp takes a row (or, where there are fewer rows than warps, a
+// part of a row's heads): its lanes form the row's cosines and sines once (in turns, in 64 bits: an fp32 product loses the
+// turn from positions of about 10^4 on) and hand them round through shared memory; then each lane keeps the turns of its
+// channels, multiplied with the norm's weight, in registers for all heads:
+//   u' = inv (x_u (w_u c) - x_v (w_v s)),   v' = inv (x_v (w_v c) + x_u (w_u s)).
+// (Turns and weights re-read from shared memory for every head cost as much as the rest: with CTAs that share rows the
+// clip of 2703 rows, 32 + 8 heads of 128 took 21.7 us, 12.0 without norm and rotation; this form AAA.)  A head is an item of
+// two V-channel vectors per lane (for the half layout the two halves of V pairs), the lanes of a head are the power of two
+// that covers it, and a warp holds 32 / lanes heads; the next heads are on their way while the present ones are worked on.
+// Rows are dealt out to the warps by the number that only the device knows, so worst-case buffers cost nothing.
 #include "ttf_paged.cuh"
+
+#include <type_traits>
 
 namespace ttf {
 
-constexpr int kRotThreads = 256;
+constexpr int kRotThreads = 128;
+constexpr int kRotCtas = 5;                        // per SM
+constexpr int kRotParts = 64;                      // parts of a row's heads at most
 
 // NI items per lane (more than one only where a head has more items than a warp has lanes)
 template <int V> struct Items { static constexpr int PER_LANE = kMaxDim / (2 * V) > 32 ? kMaxDim / (2 * V) / 32 : 1; };
@@ -28,162 +36,288 @@ template <int V> __device__ __forceinline__ void item_at(int it, int rot, int in
     e1 = halves ? rot / 2 + it * V : e0 + V;
 }
 
-template <typename T, int V, bool APPEND>
-__global__ void __launch_bounds__(kRotThreads)
-k_rotate(const __grid_constant__ RotateArgs a, int lanes)
+// a * b + c and a * b on two channels at once (one instruction of the fp32 pipe)
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "mul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+// y[] = x[] * b[] (+ c[]) over N channels
+template <int N> __device__ __forceinline__ void vmul(float (&y)[N], const float (&x)[N], const float (&b)[N]) {
+    if constexpr (N == 1) y[0] = x[0] * b[0];
+    else {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const float2 d = mul2(make_float2(x[i], x[i + 1]), make_float2(b[i], b[i + 1]));
+            y[i] = d.x; y[i + 1] = d.y;
+        }
+    }
+}
+template <int N> __device__ __forceinline__ void vfma(float (&y)[N], const float (&x)[N], const float (&b)[N], const float (&c)[N]) {
+    if constexpr (N == 1) y[0] = fmaf(x[0], b[0], c[0]);
+    else {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const float2 d = fma2(make_float2(x[i], x[i + 1]), make_float2(b[i], b[i + 1]), make_float2(c[i], c[i + 1]));
+            y[i] = d.x; y[i + 1] = d.y;
+        }
+    }
+}
+template <int N> __device__ __forceinline__ float sum_of(const float (&x)[N]) {
+    if constexpr (N == 1) return x[0];
+    else if constexpr (N == 2) return x[0] + x[1];
+    else if constexpr (N == 4) return (x[0] + x[1]) + (x[2] + x[3]);
+    else return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+}
+
+template <typename T, int V, bool APPEND, bool INTER>
+__global__ void __launch_bounds__(kRotThreads, kRotCtas)
+k_rotate(const __grid_constant__ RotateArgs a, int llanes)
 {
-    using IO = VecIO<T, V>;
-    using Raw = typename IO::Raw;
+    using Raw = typename VecIO<T, V>::Raw;
     constexpr int NI = Items<V>::PER_LANE;
-    __shared__ float2 s_turn[2][kMaxDim / 2];
-    const int tid = threadIdx.x, lane = tid & (lanes - 1);
-    const int groups = kRotThreads / lanes, grp = tid / lanes;
+    constexpr int AHEAD = 2;                               // heads of a lane on their way
+    __shared__ float2 s_turn[kRotThreads / 32][kMaxDim / 2];
+    const int ln = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lanes = 1 << llanes, lane = ln & (lanes - 1), sub = ln >> llanes, per_warp = 32 >> llanes;
     const int D = a.dim, rot = a.rot, pairs = rot >> 1;
     const int nitems = (D + 2 * V - 1) / (2 * V);
     const int Hq = a.q.heads, Hk = a.k.heads, heads = Hq + Hk + (APPEND ? a.v.heads : 0);
-    // this CTA's heads
-    const int h0 = (int)((long long)heads * blockIdx.y / gridDim.y), h1 = (int)((long long)heads * (blockIdx.y + 1) / gridDim.y);
+    float2* const turn = s_turn[warp];
+
+    int e[NI][2];                                          // this lane's channels
+    bool in[NI][2], turned[NI];
+#pragma unroll
+    for (int u = 0; u < NI; ++u) {
+        item_at<V>(lane + u * 32, rot, INTER, e[u][0], e[u][1]);
+        in[u][0] = lane + u * 32 < nitems && e[u][0] < D;
+        in[u][1] = lane + u * 32 < nitems && e[u][1] < D;
+        turned[u] = in[u][0] && e[u][0] < rot;
+    }
+    // the coordinates of the pairs ln, ln + 32, ...
+    int axis[kMaxDim / 64];
+    float freq[kMaxDim / 64];
+#pragma unroll
+    for (int i = 0; i < kMaxDim / 64; ++i) {
+        const int j = ln + 32 * i;
+        axis[i] = 0;
+        if (a.axes > 1 && j < pairs) {
+            if (a.cyclic) {
+                const int of = a.axes == 2 ? j >> 1 : j / 3, m = j - of * a.axes;
+                axis[i] = m > 0 && of < (m == 1 ? a.sec1 : a.sec2) ? m : 0;
+            } else axis[i] = j < a.sec0 ? 0 : (j < a.sec0 + a.sec1 ? 1 : 2);
+        }
+    }
 
     pdl_wait();
     int n = a.rows;
     if (APPEND) n = min(n, max(0, __ldcg(a.seq.start + a.seq.seqs)));
     else if (a.count) n = min(n, max(0, __ldcg(a.count)));
-
-    // the coordinate that this thread's pair turns with
-    int axis = 0;
-    double freq = 0.0;
-    if (tid < pairs) {
-        freq = (double)__ldcg(a.freq + tid) * 0.15915494309189533577;          // turns per position
-        if (a.axes > 1) {
-            if (a.cyclic) {
-                const int m = tid % a.axes;
-                axis = m > 0 && tid / a.axes < (m == 1 ? a.sec1 : a.sec2) ? m : 0;
-            } else axis = tid < a.sec0 ? 0 : (tid < a.sec0 + a.sec1 ? 1 : 2);
-        }
-    }
-
-    int buf = 0;
-    for (int row = blockIdx.x; row < n; row += gridDim.x, buf ^= 1) {
-        // where the row's keys and values go
-        long long k_at = 0, v_at = 0;
-        bool stored = false, there = true;
-        if (APPEND) {
-            int b = 0;                                     // sequences that end at or before this row
-            for (int s = (tid & 31); s - (tid & 31) < a.seq.seqs; s += 32)
-                b += __popc(__ballot_sync(0xffffffffu, s < a.seq.seqs && __ldcg(a.seq.start + s + 1) <= row));
-            SeqRange r = {0, 0, 0, false};
-            if (b < a.seq.seqs) r = seq_range(a.seq, b, a.cache.page);
-            const int i = row - r.first;
-            there = r.ok && i >= 0 && i < r.n;
-            bool bad = !there;
-            const int slot = r.length - r.n + i;
-            if (there && slot >= 0) {
-                const int index = quotient(slot, a.cache.page);
-                const int g = page_of(a.seq.table + (long long)b * a.seq.table_stride, index, a.cache.pages, bad);
-                const int in_page = slot - index * (int)a.cache.page.d;
-                k_at = g * a.cache.k_page + in_page * a.cache.k_row;
-                v_at = g * a.cache.v_page + in_page * a.cache.v_row;
-                stored = !bad && in_bounds(a.hdr, 7, (long long)g * a.cache.page.d + in_page, (long long)a.cache.pages * a.cache.page.d);
-            }
-            if (bad && tid == 0) report_paged(a.hdr, 2);
-        }
-        if (tid < pairs) {
-            const double turn = (double)__ldcg(a.pos + (long long)row * a.axes + axis) * freq;
-            float c, s;
-            sincospif((float)(2.0 * (turn - rint(turn))), &s, &c);
-            s_turn[buf][tid] = make_float2(c * a.factor, s * a.factor);
-        }
-        bool synced = false;                               // (the heads' loads are issued before the barrier)
-        for (int hb = h0; hb < h1; hb += groups) {
-            const int h = hb + grp;
-            const bool on = h < h1 && there;
-            const int kind = h < Hq ? 0 : (h < Hq + Hk ? 1 : 2);
-            const HeadsView& in = kind == 0 ? a.q : (kind == 1 ? a.k : a.v);
-            const int hh = h - (kind == 0 ? 0 : (kind == 1 ? Hq : Hq + Hk));
-            const T* src = reinterpret_cast<const T*>(in.data) + (long long)row * in.row + (long long)hh * in.head;
-            Raw ra[NI][2];
-            int e[NI][2];
 #pragma unroll
-            for (int u = 0; u < NI; ++u) {
-                const int it = lane + u * 32;
-                item_at<V>(it, kind == 2 ? 0 : rot, a.interleaved, e[u][0], e[u][1]);
+    for (int i = 0; i < kMaxDim / 64; ++i) freq[i] = ln + 32 * i < pairs ? __ldcg(a.freq + ln + 32 * i) : 0.f;
+
+    const int warps = gridDim.x * (kRotThreads / 32);
+    int parts = 1;                                         // of a row's heads
+    if (n > 0 && n < warps) parts = min(min(warps / n, (heads + per_warp - 1) / per_warp), kRotParts);
+    const int units = n * parts;
+    for (int unit = warp * gridDim.x + blockIdx.x; unit < units; unit += warps) {
+        const int row = parts > 1 ? unit / parts : unit, part = unit - row * parts;
+        const int h0 = parts > 1 ? heads * part / parts : 0, h1 = parts > 1 ? heads * (part + 1) / parts : heads;
+
+        float2 tn[NI][V];                                  // this lane's turns
+        bool have = false;
+        auto make_turns = [&]() {
+            __syncwarp();
 #pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    ra[u][w] = Raw{};
-                    if (on && it < nitems && e[u][w] < D) ra[u][w] = load_cg(reinterpret_cast<const Raw*>(src + e[u][w]));
+            for (int i = 0; i < kMaxDim / 64; ++i) {
+                const int j = ln + 32 * i;
+                if (j < pairs) {
+                    const double w = (double)__ldcg(a.pos + (long long)row * a.axes + axis[i]) * ((double)freq[i] * 0.15915494309189533577);
+                    float c, s;
+                    sincospif((float)(2.0 * (w - rint(w))), &s, &c);
+                    turn[j] = make_float2(c * a.factor, s * a.factor);
                 }
             }
-            if (!synced) { __syncthreads(); synced = true; }
-            T* dst = nullptr;                              // NULL: nothing to store
-            if (on && in_bounds(a.hdr, 6, (long long)row * heads + h, (long long)a.rows * heads)) {
-                if (kind == 0) dst = reinterpret_cast<T*>(a.out_q.data) + (long long)row * a.out_q.row + (long long)hh * a.out_q.head;
-                else if (!APPEND) dst = reinterpret_cast<T*>(a.out_k.data) + (long long)row * a.out_k.row + (long long)hh * a.out_k.head;
-                else if (stored) dst = kind == 1 ? reinterpret_cast<T*>(a.cache.k) + k_at + (long long)hh * a.cache.k_head
-                                                 : reinterpret_cast<T*>(a.cache.v) + v_at + (long long)hh * a.cache.v_head;
-            }
-            const void* weight = kind == 0 ? a.q_weight : (kind == 1 ? a.k_weight : nullptr);
-            float x[NI][2][V];
-            float ssq = 0.f;
+            __syncwarp();
 #pragma unroll
             for (int u = 0; u < NI; ++u)
 #pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    unpack<V>(ra[u][w], x[u][w], T{});
-#pragma unroll
-                    for (int c = 0; c < V; ++c) ssq = fmaf(x[u][w][c], x[u][w][c], ssq);
+                for (int c = 0; c < V; ++c) {
+                    const int j = (INTER ? e[u][0] >> 1 : e[u][0]) + c;
+                    tn[u][c] = turned[u] && j < pairs ? turn[j] : make_float2(1.f, 0.f);
                 }
-            if (a.q_weight || a.k_weight) {                // (uniform over the warp: its heads may be of both kinds)
-                for (int o = lanes >> 1; o > 0; o >>= 1) ssq += __shfl_xor_sync(0xffffffffu, ssq, o);
+        };
+
+        // where the row's keys and values go
+        long long k_at = 0, v_at = 0;
+        bool there = true, stored = false;
+        auto find_place = [&]() {
+            int b = 0;                                     // sequences that end at or before this row
+            for (int s = ln; s - ln < a.seq.seqs; s += 32)
+                b += __popc(__ballot_sync(0xffffffffu, s < a.seq.seqs && __ldcg(a.seq.start + s + 1) <= row));
+            SeqRange r = {0, 0, 0, false};
+            if (b < a.seq.seqs) r = seq_range(a.seq, b, a.cache.page);
+            const int i = row - r.first, slot = r.length - r.n + i;
+            there = r.ok && i >= 0 && i < r.n;
+            bool bad = !there;
+            if (there && slot >= 0) {
+                const int index = quotient(slot, a.cache.page);
+                const long long g = page_of(a.seq.table + (long long)b * a.seq.table_stride, index, a.cache.pages, bad);
+                const int in_page = slot - index * (int)a.cache.page.d;
+                k_at = g * a.cache.k_page + in_page * a.cache.k_row;
+                v_at = g * a.cache.v_page + in_page * a.cache.v_row;
+                stored = !bad && in_bounds(a.hdr, 7, g * a.cache.page.d + in_page, (long long)a.cache.pages * a.cache.page.d);
             }
-            if (weight) {
-                const float inv = 1.0f / sqrtf(ssq / (float)D + a.eps);
+            if (bad && ln == 0) report_paged(a.hdr, 2);
+        };
+
+        auto pass = [&](auto kind_of, const HeadsView& src_of, int first, const void* weight, T* to, long long to_head, bool store) {
+            constexpr int KIND = decltype(kind_of)::value;
+            const int b = max(h0, first), z = min(h1, first + src_of.heads);
+            if (b >= z) return;
+            const T* src = reinterpret_cast<const T*>(src_of.data) + (long long)row * src_of.row + (long long)(b - first + sub) * src_of.head;
+            const long long step = src_of.head << (5 - llanes);
+            int left = z - b - sub;                        // this lane group's heads are there while it is positive
+            Raw raw[AHEAD][NI][2];
+            auto fetch = [&](int ahead, Raw (&x)[NI][2]) {
 #pragma unroll
                 for (int u = 0; u < NI; ++u)
 #pragma unroll
-                    for (int w = 0; w < 2; ++w)
-                        if (lane + u * 32 < nitems && e[u][w] < D) {
-                            float wt[V];
-                            unpack<V>(load_cg(reinterpret_cast<const Raw*>(reinterpret_cast<const T*>(weight) + e[u][w])), wt, T{});
+                    for (int w = 0; w < 2; ++w) {
+                        x[u][w] = Raw{};
+                        if (left > ahead * per_warp && in[u][w]) x[u][w] = load_cg(reinterpret_cast<const Raw*>(src + e[u][w]));
+                    }
+                src += step;
+            };
 #pragma unroll
-                            for (int c = 0; c < V; ++c) x[u][w][c] *= inv * wt[c];
-                        }
+            for (int y = 0; y < AHEAD; ++y) fetch(y, raw[y]);
+            if (APPEND && !have) find_place();
+            // (with the first heads on their way)
+            if (KIND != 2 && !have) make_turns();
+            have = true;
+            if (APPEND) {
+                store = store && (KIND == 0 ? there : stored);
+                to += KIND == 0 ? 0 : (KIND == 1 ? k_at : v_at);
             }
-            if (kind != 2) {
+            to += (long long)(b - first + sub) * to_head;
+            const long long to_step = to_head << (5 - llanes);
+            // turn times weight: cu = w_u c, sv = - w_v s, cv = w_v c, su = w_u s
+            float cu[NI][V], sv[NI][V], cv[NI][V], su[NI][V];
+            if (KIND != 2) {
 #pragma unroll
                 for (int u = 0; u < NI; ++u) {
-                    if (a.interleaved) {
-                        // flat channel c of the item's 2 V: pairs of neighbours
+                    float w0[V], w1[V];
 #pragma unroll
-                        for (int c = 0; c < 2 * V; c += 2) {
-                            if (e[u][0] + c >= rot) continue;
-                            float& p0 = x[u][c / V][c % V];
-                            float& p1 = x[u][(c + 1) / V][(c + 1) % V];
-                            const float2 t = s_turn[buf][(e[u][0] + c) >> 1];
-                            const float a0 = p0, a1 = p1;
-                            p0 = a0 * t.x - a1 * t.y;
-                            p1 = a1 * t.x + a0 * t.y;
-                        }
-                    } else if (e[u][0] < pairs && e[u][1] == pairs + e[u][0]) {
+                    for (int c = 0; c < V; ++c) w0[c] = w1[c] = 1.f;
+                    if (weight) {
+                        if (in[u][0]) unpack<V>(load_cg(reinterpret_cast<const Raw*>(reinterpret_cast<const T*>(weight) + e[u][0])), w0, T{});
+                        if (in[u][1]) unpack<V>(load_cg(reinterpret_cast<const Raw*>(reinterpret_cast<const T*>(weight) + e[u][1])), w1, T{});
+                    }
 #pragma unroll
-                        for (int c = 0; c < V; ++c) {
-                            const float2 t = s_turn[buf][e[u][0] + c];
-                            const float a0 = x[u][0][c], a1 = x[u][1][c];
-                            x[u][0][c] = a0 * t.x - a1 * t.y;
-                            x[u][1][c] = a1 * t.x + a0 * t.y;
-                        }
+                    for (int c = 0; c < V; ++c) {
+                        // channels of pair c: the vectors' c, or 2c and 2c + 1 of the two vectors in a row
+                        const float wu = INTER ? (2 * c < V ? w0[2 * c % V] : w1[2 * c % V]) : w0[c];
+                        const float wv = INTER ? (2 * c + 1 < V ? w0[(2 * c + 1) % V] : w1[(2 * c + 1) % V]) : w1[c];
+                        cu[u][c] = wu * tn[u][c].x; su[u][c] = wu * tn[u][c].y;
+                        cv[u][c] = wv * tn[u][c].x; sv[u][c] = -wv * tn[u][c].y;
                     }
                 }
             }
-            if (dst) {
+#pragma unroll 1
+            for (int done = z - b; done > 0; done -= AHEAD * per_warp) {
 #pragma unroll
-                for (int u = 0; u < NI; ++u)
+                for (int y = 0; y < AHEAD; ++y) {
+                    if (done <= y * per_warp) break;       // (the same for the whole warp)
+                    const bool on = left > 0;
+                    Raw now[NI][2];
 #pragma unroll
-                    for (int w = 0; w < 2; ++w)
-                        if (lane + u * 32 < nitems && e[u][w] < D)
-                            *reinterpret_cast<Raw*>(dst + e[u][w]) = kind == 2 ? ra[u][w] : pack<V>(x[u][w], T{});
+                    for (int u = 0; u < NI; ++u) { now[u][0] = raw[y][u][0]; now[u][1] = raw[y][u][1]; }
+                    fetch(AHEAD, raw[y]);
+                    if constexpr (KIND != 2) {
+                        float x[NI][2][V];
+#pragma unroll
+                        for (int u = 0; u < NI; ++u)
+#pragma unroll
+                            for (int w = 0; w < 2; ++w) unpack<V>(now[u][w], x[u][w], T{});
+                        float inv[V];
+                        inv[0] = 1.f;
+                        if (weight) {
+                            float part[V];
+#pragma unroll
+                            for (int c = 0; c < V; ++c) part[c] = 0.f;
+#pragma unroll
+                            for (int u = 0; u < NI; ++u)
+#pragma unroll
+                                for (int w = 0; w < 2; ++w) vfma<V>(part, x[u][w], x[u][w], part);
+                            float ssq = sum_of<V>(part);
+                            if (llanes == 3) {             // (heads of 128 channels in bf16)
+                                ssq += __shfl_xor_sync(0xffffffffu, ssq, 4);
+                                ssq += __shfl_xor_sync(0xffffffffu, ssq, 2);
+                                ssq += __shfl_xor_sync(0xffffffffu, ssq, 1);
+                            } else
+                                for (int o = lanes >> 1; o > 0; o >>= 1) ssq += __shfl_xor_sync(0xffffffffu, ssq, o);
+                            inv[0] = rsqrtf(fmaf(ssq, a.inv_dim, a.eps));
+                        }
+#pragma unroll
+                        for (int c = 1; c < V; ++c) inv[c] = inv[0];
+#pragma unroll
+                        for (int u = 0; u < NI; ++u) {
+                            float pu[V], pv[V], t0[V], t1[V], qu[V], qv[V];
+#pragma unroll
+                            for (int c = 0; c < V; ++c) {
+                                pu[c] = INTER ? x[u][2 * c / V][2 * c % V] : x[u][0][c];
+                                pv[c] = INTER ? x[u][(2 * c + 1) / V][(2 * c + 1) % V] : x[u][1][c];
+                            }
+                            if (weight) { vmul<V>(pu, pu, inv); vmul<V>(pv, pv, inv); }
+#pragma unroll
+                            for (int c = 0; c < V; ++c) { qu[c] = pu[c]; qv[c] = pv[c]; }
+                            if (rot < D) {                 // channels that do not turn: their neighbour, whatever it holds, plays no part
+#pragma unroll
+                                for (int c = 0; c < V; ++c) {
+                                    const bool t = turned[u] && (!INTER || (e[u][0] >> 1) + c < pairs);
+                                    qu[c] = t ? qu[c] : 0.f; qv[c] = t ? qv[c] : 0.f;
+                                }
+                            }
+                            vmul<V>(t0, qv, sv[u]);
+                            vmul<V>(t1, qu, su[u]);
+                            vfma<V>(t0, pu, cu[u], t0);
+                            vfma<V>(t1, pv, cv[u], t1);
+#pragma unroll
+                            for (int c = 0; c < V; ++c) {
+                                if (INTER) { x[u][2 * c / V][2 * c % V] = t0[c]; x[u][(2 * c + 1) / V][(2 * c + 1) % V] = t1[c]; }
+                                else { x[u][0][c] = t0[c]; x[u][1][c] = t1[c]; }
+                            }
+                        }
+#pragma unroll
+                        for (int u = 0; u < NI; ++u) { now[u][0] = pack<V>(x[u][0], T{}); now[u][1] = pack<V>(x[u][1], T{}); }
+                    }
+                    if (on && store && in_bounds(a.hdr, 6, (long long)(row + 1) * heads - 1, (long long)a.rows * heads)) {
+#pragma unroll
+                        for (int u = 0; u < NI; ++u)
+#pragma unroll
+                            for (int w = 0; w < 2; ++w)
+                                if (in[u][w]) *reinterpret_cast<Raw*>(to + e[u][w]) = now[u][w];
+                    }
+                    to += to_step;
+                    left -= per_warp;
+                }
             }
-        }
-        if (!synced) __syncthreads();
+        };
+        pass(std::integral_constant<int, 0>{}, a.q, 0, a.q_weight, reinterpret_cast<T*>(a.out_q.data) + (long long)row * a.out_q.row, a.out_q.head, true);
+        if (APPEND) {
+            pass(std::integral_constant<int, 1>{}, a.k, Hq, a.k_weight, reinterpret_cast<T*>(a.cache.k), a.cache.k_head, true);
+            pass(std::integral_constant<int, 2>{}, a.v, Hq + Hk, nullptr, reinterpret_cast<T*>(a.cache.v), a.cache.v_head, true);
+        } else
+            pass(std::integral_constant<int, 1>{}, a.k, Hq, a.k_weight, reinterpret_cast<T*>(a.out_k.data) + (long long)row * a.out_k.row, a.out_k.head, true);
     }
     pdl_launch_dependents();
 }
@@ -205,16 +339,15 @@ static cudaError_t launch_rotate_v(const RotateArgs& a, cudaStream_t st) {
     if constexpr (V > 1) {
         if (!ok) return launch_rotate_v<T, APPEND, V / 2>(a, st);
     }
-    int lanes = 1;
-    while (lanes < 32 && lanes * 2 * V < a.dim) lanes *= 2;
-    const int heads = a.q.heads + a.k.heads + (APPEND ? a.v.heads : 0), groups = kRotThreads / lanes;
-    const int places = sm_count() * 6;
-    const int most = (heads + groups - 1) / groups;        // CTAs that can share a row
-    int split = places / a.rows;
-    if (split > most) split = most;
-    if (split < 1) split = 1;
-    const int gx = a.rows < places ? a.rows : places;
-    return launch_pdl(k_rotate<T, V, APPEND>, dim3(gx, split), dim3(kRotThreads), st, a, lanes);
+    int ll = 0;
+    while (ll < 5 && (2 * V << ll) < a.dim) ++ll;
+    const int heads = a.q.heads + a.k.heads + (APPEND ? a.v.heads : 0), per_warp = 32 >> ll;
+    // a warp per row, or per few heads of a row where that fills the SMs
+    const long long most = (long long)a.rows * ((heads + per_warp - 1) / per_warp), warps = kRotThreads / 32;
+    long long ctas = (most + warps - 1) / warps;
+    if (ctas > sm_count() * kRotCtas) ctas = sm_count() * kRotCtas;
+    return a.interleaved ? launch_pdl(k_rotate<T, V, APPEND, true>, dim3((unsigned)ctas), dim3(kRotThreads), st, a, ll)
+                         : launch_pdl(k_rotate<T, V, APPEND, false>, dim3((unsigned)ctas), dim3(kRotThreads), st, a, ll);
 }
 cudaError_t launch_rotate(const RotateArgs& a, int dtype, bool append, cudaStream_t st) {
     if (a.rows < 1) return cudaSuccess;
