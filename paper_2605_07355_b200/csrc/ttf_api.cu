@@ -66,6 +66,17 @@ cudaError_t ensure_dynamic_smem(const void* func, size_t bytes) {
     return e;
 }
 
+cudaError_t allow_large_cluster(const void* func) {
+    static FuncAttrTable allowed;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (!allowed.needs(func, dev, 1)) return cudaSuccess;
+    e = cudaFuncSetAttribute(func, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) allowed.forget(func, dev);
+    return e;
+}
+
 static std::atomic<int> g_wait_limit{1 << 18};
 static std::atomic<int> g_wait_tx_extra{0};
 int wait_poll_limit() { return g_wait_limit.load(); }

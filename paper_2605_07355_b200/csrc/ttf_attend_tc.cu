@@ -447,23 +447,31 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
         __syncwarp();
         cluster_arrive();
         cluster_wait();
-        // rows row % split == rank of both tiles, four channels per thread
+        // rows row % split == rank of both tiles: first every rank's maxima and sums, then four channels per thread
         constexpr int Q4 = DP / 4;
-        for (int e = tid; e < 2 * (kAtRows >> lsplit) * Q4; e += kAtThreads) {
-            const int d = (e % Q4) * 4, x = (e / Q4) & 1, row = ((e / Q4) >> 1 << lsplit) + rank;
+        const int mine = 2 * (kAtRows >> lsplit);          // row i of them: tile i & 1, row (i >> 1) * split + rank
+        float* const s_f = reinterpret_cast<float*>(smem) + S::ML + 4 * kAtRows;              // [i][rank]: maxima, then sums
+        for (int e = tid; e < mine << lsplit; e += kAtThreads) {
+            const int p = e & (split - 1), i = e >> lsplit, at = S::ML + (i & 1) * kAtRows + ((i >> 1) << lsplit) + rank;
+            s_f[e] = ld_cluster_f32_(cluster_addr(base_addr + (uint32_t)at * 4, p));
+            s_f[2 * kAtRows + e] = ld_cluster_f32_(cluster_addr(base_addr + (uint32_t)(at + 2 * kAtRows) * 4, p));
+        }
+        __syncthreads();
+        for (int e = tid; e < mine * Q4; e += kAtThreads) {
+            const int i = e / Q4, d = (e - i * Q4) * 4, x = i & 1, row = ((i >> 1) << lsplit) + rank;
             if (row >= ntok[x] * a.group || d >= a.cache.dim) continue;
-            const uint32_t at_m = base_addr + (uint32_t)(S::ML + x * kAtRows + row) * 4, at_l = at_m + 2 * kAtRows * 4;
             const uint32_t at_o = base_addr + (uint32_t)((x * kAtRows + row) * S::OP + d) * 4;
+            const float* const fm = s_f + (i << lsplit);
             float m = -INFINITY;
-            for (int p = 0; p < split; ++p) m = fmaxf(m, ld_cluster_f32_(cluster_addr(at_m, p)));
+            for (int p = 0; p < split; ++p) m = fmaxf(m, fm[p]);
             const float ref = m == -INFINITY ? 0.f : m;
             float l = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
             for (int p = 0; p < split; ++p) {
-                const float lp = ld_cluster_f32_(cluster_addr(at_l, p));
-                if (lp == 0.f) continue;                   // that rank saw nothing of the row
-                const float f = exp2_approx(ld_cluster_f32_(cluster_addr(at_m, p)) - ref);
                 const float4 v = ld_cluster_f32x4(cluster_addr(at_o, p));
+                const float lp = fm[2 * kAtRows + p], f = exp2_approx(fm[p] - ref);
+                if (lp == 0.f) continue;                   // that rank saw nothing of the row
                 l = fmaf(f, lp, l);
                 o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
             }
@@ -474,6 +482,7 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
             if (in_bounds(a.hdr, 8, (long long)r.first + token, a.seq.rows))
                 *reinterpret_cast<uint2*>(reinterpret_cast<bf16_t*>(a.out.data) + (long long)(r.first + token) * a.out.row + (long long)head * a.out.head + d) = w;
         }
+        __syncwarp();
         cluster_arrive();                                  // nobody leaves while its sums may be read
         cluster_wait();
     }
@@ -496,14 +505,16 @@ static bool tma_ok(const void* p, long long s0, long long s1, long long s2) {
     auto fine = [](long long s) { return s >= 0 && s % 8 == 0 && s < (1LL << 38); };
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && fine(s0) && fine(s1) && fine(s2);
 }
+bool cache_maps_fit(const AttendArgs& a) {
+    return tma_ok(a.cache.k, a.cache.k_page, a.cache.k_row, a.cache.k_head) &&
+           tma_ok(a.cache.v, a.cache.v_page, a.cache.v_row, a.cache.v_head) && encode_fn() != nullptr;
+}
 
 bool attend_tc_takes(const AttendArgs& a, int dtype) {
     const int page = (int)a.cache.page.d;
     return dtype == TTF_DTYPE_BF16 && a.cache.dim % 8 == 0 && a.cache.dim <= 128 && a.group <= kAtRows && a.scale > 0.f &&
            page % 8 == 0 && (page <= kAtSlots || page % kAtSlots == 0) &&
-           tma_ok(a.q.data, a.q.row, a.q.head, 0) && tma_ok(a.cache.k, a.cache.k_page, a.cache.k_row, a.cache.k_head) &&
-           tma_ok(a.cache.v, a.cache.v_page, a.cache.v_row, a.cache.v_head) && tma_ok(a.out.data, a.out.row, a.out.head, 0) &&
-           encode_fn() != nullptr;
+           tma_ok(a.q.data, a.q.row, a.q.head, 0) && tma_ok(a.out.data, a.out.row, a.out.head, 0) && cache_maps_fit(a);
 }
 
 // a map over axes of `n` elements with strides of `s` elements (0: an axis of one element, whose stride does not matter)
@@ -517,6 +528,13 @@ static bool encode(CUtensorMap* m, const void* data, int rank, const long long* 
                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_cache_map(CUtensorMap* m, const AttendArgs& a, bool values, int rows) {
+    const long long n[4] = {a.cache.dim, (int)a.cache.page.d, a.cache.heads, a.cache.pages};
+    const long long s[4] = {1, values ? a.cache.v_row : a.cache.k_row, values ? a.cache.v_head : a.cache.k_head, values ? a.cache.v_page : a.cache.k_page};
+    const int b[4] = {64, rows, 1, 1};
+    return encode(m, values ? a.cache.v : a.cache.k, 4, n, s, b);
+}
+
 template <int DP> static cudaError_t launch_tc_t(const AttendArgs& a, cudaStream_t st) {
     using S = AttendShape<DP>;
     const int page = (int)a.cache.page.d, per = kAtRows / a.group;
@@ -527,12 +545,7 @@ template <int DP> static cudaError_t launch_tc_t(const AttendArgs& a, cudaStream
         const int b[3] = {64, a.group, per};
         if (!encode(&maps.q, a.q.data, 3, n, s, b)) return cudaErrorInvalidValue;
     }
-    for (int kv = 0; kv < 2; ++kv) {
-        const long long n[4] = {a.cache.dim, page, a.cache.heads, a.cache.pages};
-        const long long s[4] = {1, kv ? a.cache.v_row : a.cache.k_row, kv ? a.cache.v_head : a.cache.k_head, kv ? a.cache.v_page : a.cache.k_page};
-        const int b[4] = {64, box, 1, 1};
-        if (!encode(kv ? &maps.v : &maps.k, kv ? a.cache.v : a.cache.k, 4, n, s, b)) return cudaErrorInvalidValue;
-    }
+    if (!make_cache_map(&maps.k, a, false, box) || !make_cache_map(&maps.v, a, true, box)) return cudaErrorInvalidValue;
     const void* fn = reinterpret_cast<const void*>(k_attend_tc<DP>);
     const size_t smem = S::SMEM + 1024;
     cudaError_t e = ensure_dynamic_smem(fn, smem);

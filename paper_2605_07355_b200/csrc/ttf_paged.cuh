@@ -2,6 +2,8 @@
 // sequences that the kernels take, and the look-ups in them.
 #pragma once
 
+#include <cuda.h>
+
 #include "../../include/ttf.h"
 #include "ttf_internal.cuh"
 
@@ -72,6 +74,13 @@ struct AttendArgs {
 cudaError_t launch_attend(const AttendArgs& a, int dtype, cudaStream_t st);
 bool attend_tc_takes(const AttendArgs& a, int dtype);
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t st);
+bool attend_few_takes(const AttendArgs& a, int dtype);
+cudaError_t launch_attend_few(const AttendArgs& a, cudaStream_t st);
+// TMA tiles of the cache: 64 channels x `rows` slots of one head and page, 128-byte swizzle, zeros beyond the head
+bool cache_maps_fit(const AttendArgs& a);
+bool make_cache_map(CUtensorMap* m, const AttendArgs& a, bool values, int rows);
+bool attend_mma_takes(const AttendArgs& a, int dtype);
+cudaError_t launch_attend_mma(const AttendArgs& a, cudaStream_t st);
 cudaError_t launch_attend_simple(const AttendArgs& a, int dtype, cudaStream_t st);
 
 // Upper bound on the tiles of a call (the host does not know how the rows are spread over the sequences), and the CTAs of a
@@ -175,12 +184,13 @@ __device__ __forceinline__ int tiles_of(int n, int group, int rows, int per) {
 }
 __device__ __forceinline__ bool find_tile(const AttendArgs& a, int rows, int per, int index, bool report, Tile& t) {
     const int lane = threadIdx.x & 31;
-    int total = 0;
+    int total = 0, c = 0;
     bool bad = false;
+    SeqRange r = {0, 0, 0, false};
     for (int s0 = 0; s0 < a.seq.seqs; s0 += 32) {
-        int c = 0;
+        c = 0;
         if (s0 + lane < a.seq.seqs) {
-            const SeqRange r = seq_range(a.seq, s0 + lane, a.cache.page);
+            r = seq_range(a.seq, s0 + lane, a.cache.page);
             bad |= !r.ok;
             c = tiles_of(r.n, a.group, rows, per);
         }
@@ -190,11 +200,12 @@ __device__ __forceinline__ bool find_tile(const AttendArgs& a, int rows, int per
     int want = total - 1 - index;
     if (want < 0) return false;
     for (int s0 = 0; s0 < a.seq.seqs; s0 += 32) {
-        int c = 0;
-        SeqRange r = {0, 0, 0, false};
-        if (s0 + lane < a.seq.seqs) {
-            r = seq_range(a.seq, s0 + lane, a.cache.page);
-            c = tiles_of(r.n, a.group, rows, per);
+        if (a.seq.seqs > 32) {                     // (up to 32 sequences are still in registers)
+            c = 0;
+            if (s0 + lane < a.seq.seqs) {
+                r = seq_range(a.seq, s0 + lane, a.cache.page);
+                c = tiles_of(r.n, a.group, rows, per);
+            }
         }
         int upto = c;                              // inclusive scan
 #pragma unroll
