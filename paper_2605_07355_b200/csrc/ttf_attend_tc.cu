@@ -7,8 +7,8 @@
 // slots in blocks of (up to) 128:
 //   warp 8       TMA: the pages of a block, keys then values, into a ring of [128 slots x DP channels] slots (128-byte swizzle;
 //                channels beyond the head arrive as zeros)
-//   warp 9       tcgen05.mma: S0 = Q0 K^T, S1 = Q1 K^T (both operands in shared memory), O0 += P0 V, O1 += P1 V (P in tensor
-//                memory, V read as the transposed operand)
+//   warps 9, 10  tcgen05.mma, one thread per tile: S = Q K^T (both operands in shared memory), O += P V (P in tensor memory, V
+//                read as the transposed operand)
 //   warps 0 - 3  softmax of tile 0, one row per thread; warps 4 - 7 the same for tile 1
 // While one tile's weights are formed the other tile's products run: O0 += P0 V(j), S0 = Q0 K(j+1)^T, O1 += P1 V(j),
 // S1 = Q1 K(j+1)^T.  P takes the place of its scores in tensor memory, so the next scores of a tile are only asked for when the
@@ -36,7 +36,8 @@ namespace ttf {
 
 constexpr int kAtRows = 128;                       // rows of a tile = tensor-memory lanes
 constexpr int kAtSlots = 128;                      // slots of a block
-constexpr int kAtThreads = 320;
+constexpr int kAtHalf = 64;                        // slots whose scores and weights are handed over at a time
+constexpr int kAtThreads = 352;
 
 template <int DP> struct AttendShape {
     static constexpr int HALVES = DP / 64;                         // 128-byte columns of a row
@@ -110,6 +111,11 @@ template <int N> __device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[N]) 
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -133,7 +139,7 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
 {
     using S = AttendShape<DP>;
     extern __shared__ unsigned char at_raw[];
-    __shared__ uint64_t bar_q, bar_full[S::RING], bar_empty[S::RING], bar_s[2], bar_p[2], bar_pv[2], bar_end;
+    __shared__ uint64_t bar_q, bar_full[S::RING], bar_empty[S::RING], bar_raw, bar_s[2][2], bar_p[2][2], bar_pv[2], bar_o[2], bar_end;
     __shared__ uint32_t s_tmem;
     __shared__ int s_err;
 
@@ -172,10 +178,9 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
     const uint32_t base_addr = (smem_u32(at_raw) + 1023u) & ~1023u;
     unsigned char* const smem = at_raw + (base_addr - smem_u32(at_raw));
     if (tid == 0) {
-        mbar_init(&bar_q, 1);
-        mbar_init(&bar_end, 1);
-        for (int s = 0; s < S::RING; ++s) { mbar_init(&bar_full[s], 1); mbar_init(&bar_empty[s], 1); }
-        for (int x = 0; x < 2; ++x) { mbar_init(&bar_s[x], 1); mbar_init(&bar_p[x], 4); mbar_init(&bar_pv[x], 1); }
+        mbar_init(&bar_q, 1); mbar_init(&bar_raw, 1); mbar_init(&bar_end, 2);
+        for (int s = 0; s < S::RING; ++s) { mbar_init(&bar_full[s], 1); mbar_init(&bar_empty[s], 2); }
+        for (int x = 0; x < 2; ++x) { for (int b = 0; b < 2; ++b) { mbar_init(&bar_s[x][b], 1); mbar_init(&bar_p[x][b], 4); } mbar_init(&bar_pv[x], 1); mbar_init(&bar_o[x], 1); }
         mbar_init_fence();
         s_err = 0;
         tensormap_prefetch(&maps.q); tensormap_prefetch(&maps.k); tensormap_prefetch(&maps.v);
@@ -196,6 +201,15 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
     const uint32_t tmem = s_tmem;
     auto failed = [&]() { return *(volatile int*)&s_err != 0; };
     auto give_up = [&]() { atomicExch(&s_err, 1); };
+    // (a role that gives up is noticed by the others, or their own waits run out)
+    auto wait = [&](uint64_t* bar, int parity) {
+        for (int i = 0; i < limit; ++i) {
+            if (mbar_try_wait(bar, parity)) return true;
+            if ((i & 63) == 63 && failed()) break;
+        }
+        give_up();
+        return false;
+    };
 
     if (warp == 8) {
         // ---- producer -------------------------------------------------------------------------------------------
@@ -209,7 +223,7 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
         }
         const int* const table = a.seq.table + (long long)t.seq * a.seq.table_stride;
         const int page = (int)a.cache.page.d;
-        int issued = 0;
+        int issued = 0, raw = 0;
         auto page_id = [&](int j) {                        // lane = page of the block (box_rows rows each)
             const int s0 = j * block + lane * box_rows;
             if (lane * box_rows >= block || j >= j_hi || s0 >= hi_u || s0 + box_rows <= lo_u) return -1;
@@ -220,22 +234,37 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
             const int next = page_id(j + 1);
             const uint32_t bytes = (uint32_t)(__popc(__ballot_sync(0xffffffffu, id >= 0)) * box_rows * 128 * S::HALVES);
             const int row = j * block + lane * box_rows - quotient(j * block + lane * box_rows, a.cache.page) * page;
+            const int s0 = j * block;
+            const bool edge = s0 < lo_u || s0 + block > hi_u;              // some slots are seen by no row of the CTA
             bool ok = true;
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
                 const int idx = 2 * (j - j_lo) + kv, slot = idx % S::RING;
-                if (idx >= S::RING && !mbar_wait(&bar_empty[slot], ((idx / S::RING) & 1) ^ 1, limit)) { give_up(); ok = false; }
-                ok = __all_sync(0xffffffffu, ok && !failed());
+                ok = __all_sync(0xffffffffu, idx < S::RING || wait(&bar_empty[slot], ((idx / S::RING) & 1) ^ 1));
                 if (!ok) break;
-                if (lane == 0) mbar_arrive_expect_tx(&bar_full[slot], bytes + (uint32_t)a.tx_extra);
+                uint64_t* const bar = kv && edge ? &bar_raw : &bar_full[slot];
+                if (lane == 0) mbar_arrive_expect_tx(bar, bytes + (uint32_t)a.tx_extra);
                 __syncwarp();
+                unsigned char* const to = smem + 2 * S::TILE + slot * S::TILE;
                 if (id >= 0) {
-                    unsigned char* dst = smem + 2 * S::TILE + slot * S::TILE + lane * box_rows * 128;
+                    unsigned char* dst = to + lane * box_rows * 128;
                     const CUtensorMap* map = kv ? &maps.v : &maps.k;
 #pragma unroll
-                    for (int h = 0; h < S::HALVES; ++h) tma_load_4d(dst + h * S::COL, map, h * 64, row, hk, id, &bar_full[slot]);
+                    for (int h = 0; h < S::HALVES; ++h) tma_load_4d(dst + h * S::COL, map, h * 64, row, hk, id, bar);
                 }
                 issued = idx + 1;
+                if (kv && edge) {                          // their values: zeros, whatever the page (or an earlier block) holds
+                    ok = __all_sync(0xffffffffu, wait(&bar_raw, raw & 1));
+                    if (!ok) break;
+                    ++raw;
+                    for (int i = lane; i < block * 8 * S::HALVES; i += 32) {
+                        const int h = i / (block * 8), o = i - h * (block * 8), at = s0 + (o >> 3);
+                        if (at < lo_u || at >= hi_u) *reinterpret_cast<uint4*>(to + h * S::COL + o * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar_full + slot);
+                }
             }
             if (!ok) break;
             id = next;
@@ -243,83 +272,68 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
         if (__any_sync(0xffffffffu, bad) && lane == 0) report_paged(a.hdr, 2);
         if (failed()) {                                    // copies in flight land before the CTA may leave
             if (j_lo < j_hi) mbar_wait(&bar_q, 0, limit);
+            mbar_wait(&bar_raw, raw & 1, limit);
             for (int i = issued > S::RING ? issued - S::RING : 0; i < issued; ++i)
                 mbar_wait(&bar_full[i % S::RING], (i / S::RING) & 1, limit);
         }
-    } else if (warp == 9) {
-        // ---- products ---------------------------------------------------------------------------------------------
-        constexpr uint32_t id_s = idesc_attend(kAtSlots, false), id_o = idesc_attend(DP, true);
-        bool ok = true;
-        auto wait = [&](uint64_t* bar, int parity) {
-            if (ok && !__all_sync(0xffffffffu, !failed() && mbar_wait(bar, parity, limit))) { ok = false; give_up(); }
-        };
-        auto ring = [&](int idx) { return base_addr + 2 * S::TILE + (uint32_t)(idx % S::RING) * S::TILE; };
-        auto scores = [&](int x, int j) {                  // S_x = Q_x K(j)^T
-            if (lane == 0) {
-                const uint64_t dq = smem_desc_sw128(base_addr + x * S::TILE), dk = smem_desc_sw128(ring(2 * (j - j_lo)));
+    } else if (warp >= 9) {
+        // ---- products: one thread per tile ------------------------------------------------------------------------
+        if (lane == 0) {
+            constexpr uint32_t id_s = idesc_attend(kAtHalf, false), id_o = idesc_attend(DP, true);
+            const int x = warp - 9, t_lo = jt_lo[x], t_hi = jt_hi[x];
+            const uint64_t dq = smem_desc_sw128(base_addr + x * S::TILE);
+            const uint64_t dk0 = smem_desc_sw128(base_addr + 2 * S::TILE), dv0 = smem_desc_sw128_mn(base_addr + 2 * S::TILE, S::COL);
+            // S = Q K^T of half a block's slots, keys in ring slot `at`
+            auto scores = [&](int half, int at) {
+                tc_fence_after();
+                const uint64_t dk = dk0 + (uint64_t)((at * S::TILE + half * (kAtHalf * 128)) >> 4);
 #pragma unroll
                 for (int k = 0; k < DP / 16; ++k) {
-                    const uint64_t at = (uint64_t)(((k / 4) * S::COL + (k % 4) * 32) >> 4);
-                    umma_bf16(tmem + x * 128, dq + at, dk + at, id_s, k > 0);
+                    const uint64_t step = (uint64_t)(((k / 4) * S::COL + (k % 4) * 32) >> 4);
+                    umma_bf16(tmem + x * 128 + half * kAtHalf, dq + step, dk + step, id_s, k > 0);
                 }
-                umma_commit(&bar_s[x]);
-            }
-            __syncwarp();
-        };
-        auto weigh = [&](int x, int j) {                   // O_x += P_x V(j)
-            if (lane == 0) {
-                const uint64_t dv = smem_desc_sw128_mn(ring(2 * (j - j_lo) + 1), S::COL);
-#pragma unroll
-                for (int k = 0; k < kAtSlots / 16; ++k)
-                    umma_bf16_ts(tmem + S::O_COL + x * DP, tmem + x * 128 + k * 8, dv + (uint64_t)(k * (16 * 128 >> 4)), id_o,
-                                 k > 0 || j > jt_lo[x]);
-                umma_commit(&bar_pv[x]);
-            }
-            __syncwarp();
-        };
-        auto done_with = [&](int idx) { if (lane == 0) umma_commit(&bar_empty[idx % S::RING]); __syncwarp(); };
-        auto has = [&](int x, int j) { return j >= jt_lo[x] && j < jt_hi[x]; };
-        if (j_lo < j_hi) {
-            wait(&bar_q, 0);
-            wait(&bar_full[0], 0);
-            tc_fence_after();
+                umma_commit(&bar_s[x][half]);
+            };
+            bool ok = j_lo < j_hi && wait(&bar_q, 0) && wait(&bar_full[0], 0);
             if (ok) {
-                for (int x = 0; x < 2; ++x) if (has(x, j_lo)) scores(x, j_lo);
-                done_with(0);
+                if (j_lo >= t_lo && j_lo < t_hi) { scores(0, 0); scores(1, 0); umma_commit(&bar_empty[0]); }
+                else mbar_arrive(&bar_empty[0]);
             }
-        }
-        for (int j = j_lo; j < j_hi && ok; ++j) {
-            const int iv = 2 * (j - j_lo) + 1, ik = iv + 1;
-            wait(&bar_full[iv % S::RING], (iv / S::RING) & 1);
-            // values of slots that no row of the CTA sees
-            const int s0 = j * block;
-            if (ok && (s0 < lo_u || s0 + block > hi_u)) {
-                const int head = max(0, lo_u - s0), tail = min(block, hi_u - s0);
-                unsigned char* v = smem + (ring(iv) - base_addr);
-                for (int i = lane; i < block * 8 * S::HALVES; i += 32) {
-                    const int h = i / (block * 8), o = i - h * (block * 8), row = o >> 3;
-                    if (row < head || row >= tail) *reinterpret_cast<uint4*>(v + h * S::COL + o * 16) = make_uint4(0, 0, 0, 0);
-                }
-                fence_async_smem();
-                __syncwarp();
-            }
+            int slot = 0, phase = 0;                       // keys of block j
+            for (int j = j_lo; j < j_hi && ok; ++j) {
+                int vs = slot + 1, vp = phase;             // its values
+                if (vs == S::RING) { vs = 0; vp ^= 1; }
+                slot = vs + 1; phase = vp;                 // the next block's keys
+                if (slot == S::RING) { slot = 0; phase ^= 1; }
+                const bool here = j >= t_lo && j < t_hi, next = j + 1 >= t_lo && j + 1 < t_hi;
+                if (!(ok = wait(&bar_full[vs], vp))) break;
+                if (!here) mbar_arrive(&bar_empty[vs]);
+                const uint64_t dv = dv0 + (uint64_t)(vs * (S::TILE >> 4));
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                if (has(x, j)) {
-                    wait(&bar_p[x], (j - jt_lo[x]) & 1);
-                    tc_fence_after();
-                    if (ok) weigh(x, j);
-                }
-                if (x == 1) done_with(iv);
-                if (j + 1 < j_hi) {
-                    if (x == 0) wait(&bar_full[ik % S::RING], (ik / S::RING) & 1);
-                    if (has(x, j)) wait(&bar_pv[x], (j - jt_lo[x]) & 1);
-                    tc_fence_after();
-                    if (has(x, j + 1) && ok) scores(x, j + 1);
-                    if (x == 1) done_with(ik);
+                for (int half = 0; half < 2; ++half) {
+                    if (here) {                            // O += P V(j)
+                        if (!(ok = wait(&bar_p[x][half], (j - t_lo) & 1))) break;
+                        tc_fence_after();
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            umma_bf16_ts(tmem + S::O_COL + x * DP, tmem + x * 128 + half * kAtHalf + k * 8,
+                                         dv + (uint64_t)((half * kAtHalf + k * 16) * 128 >> 4), id_o, k > 0 || half > 0 || j > t_lo);
+                        umma_commit(&bar_pv[x]);
+                        if (half) umma_commit(&bar_empty[vs]);
+                    }
+                    if (j + 1 < j_hi) {
+                        if (half == 0 && !(ok = wait(&bar_full[slot], phase))) break;
+                        // (P is in the place of S: the product has to be through before the next scores come there)
+                        if (here && !(ok = wait(&bar_pv[x], half))) break;
+                        if (next) scores(half, slot);
+                        if (half) { if (next) umma_commit(&bar_empty[slot]); else mbar_arrive(&bar_empty[slot]); }
+                    }
                 }
             }
+            umma_commit(&bar_o[x]);                        // (a barrier of its own: two phases of bar_pv may pass unseen)
+            umma_commit(&bar_end);
         }
+        __syncwarp();
     } else {
         // ---- softmax: one row per thread ----------------------------------------------------------------------------
         const int x = warp >> 2, row = (warp & 3) * 32 + lane;
@@ -333,67 +347,68 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
         const float c = a.scale * 1.4426950408889634f;
         float m = -INFINITY, l = 0.f;
         bool ok = true;
-        for (int j = jt_lo[x]; j < jt_hi[x]; ++j) {
-            const int n = j - jt_lo[x];
-            if (!__all_sync(0xffffffffu, !failed() && mbar_wait(&bar_s[x], n & 1, limit))) { give_up(); ok = false; break; }
+        const int n = 2 * (jt_hi[x] - jt_lo[x]);           // halves of blocks
+        for (int i = 0; i < n; ++i) {
+            const int b = i & 1, parity = (i >> 1) & 1;
+            if (!__all_sync(0xffffffffu, wait(&bar_s[x][b], parity))) { ok = false; break; }
             tc_fence_after();
-            uint32_t s[128];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) tmem_ld32(s_at + i * 32, s + i * 32);
+            uint32_t s[kAtHalf];
+            const uint32_t sb = s_at + b * kAtHalf;
+            tmem_ld32(sb, s);
+            tmem_ld32(sb + 32, s + 32);
             tmem_ld_wait(s);
-            const int s0 = j * block;
-            if (block < kAtSlots || s0 < all_lo || s0 + kAtSlots > all_hi) {
-                const int lo = mine.lo - s0, hi = min(mine.hi - s0, block);
+            const int s0 = (jt_lo[x] + (i >> 1)) * block + b * kAtHalf;
+            if (block < kAtSlots || s0 < all_lo || s0 + kAtHalf > all_hi) {
+                const int lo = mine.lo - s0, hi = min(mine.hi - s0, block - b * kAtHalf);
 #pragma unroll
-                for (int i = 0; i < 128; ++i) s[i] = i >= lo && i < hi ? s[i] : 0xff800000u;
+                for (int e = 0; e < kAtHalf; ++e) s[e] = e >= lo && e < hi ? s[e] : 0xff800000u;
             }
             float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int i = 0; i < 128; i += 8)
+            for (int e = 0; e < kAtHalf; e += 8)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    mx[e] = fmaxf(mx[e], fmaxf(__uint_as_float(s[i + e]), __uint_as_float(s[i + 4 + e])));
-            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+                for (int y = 0; y < 4; ++y) mx[y] = max3(mx[y], __uint_as_float(s[e + 2 * y]), __uint_as_float(s[e + 2 * y + 1]));
+            const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * c;
             const bool grown = top > m + 8.f;              // (m = -inf: any number is)
             if (__any_sync(0xffffffffu, grown)) {
                 const float m1 = grown ? top : m;
                 const float f = m == m1 ? 1.f : exp2_approx(m - m1);
                 m = m1;
                 l *= f;
-                if (n > 0) {
+                if (i > 0) {                               // O, once the product of the half before has been added to it
+                    if (!__all_sync(0xffffffffu, wait(&bar_pv[x], b ^ 1))) { ok = false; break; }
+                    tc_fence_after();
 #pragma unroll 1
-                    for (int i = 0; i < DP; i += 32) {
+                    for (int d = 0; d < DP; d += 32) {
                         uint32_t o[32];
-                        tmem_ld32(o_at + i, o);
+                        tmem_ld32(o_at + d, o);
                         tmem_ld_wait(o);
 #pragma unroll
                         for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                        tmem_st32(o_at + i, o);
+                        tmem_st32(o_at + d, o);
                     }
                 }
             }
             const float ref = m == -INFINITY ? 0.f : m;
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            const float2 c2 = make_float2(c, c), ref2 = make_float2(-ref, -ref);
+            float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            uint32_t p[32];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t p[32];
-#pragma unroll
-                for (int i = 0; i < 64; i += 2) {
-                    const float p0 = exp2_approx(fmaf(__uint_as_float(s[h * 64 + i]), c, -ref));
-                    const float p1 = exp2_approx(fmaf(__uint_as_float(s[h * 64 + i + 1]), c, -ref));
-                    sum[(i & 2)] += p0; sum[(i & 2) + 1] += p1;
-                    p[i / 2] = bf16_pair(p0, p1);
-                }
-                tmem_st32(s_at + h * 32, p);
+            for (int e = 0; e < 32; ++e) {
+                const float2 t = fma2(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), c2, ref2);
+                const float2 w = make_float2(exp2_approx(t.x), exp2_approx(t.y));
+                sum[e & 1] = add2(sum[e & 1], w);
+                p[e] = bf16_pair(w.x, w.y);
             }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            tmem_st32(sb, p);
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bar_p[x]);
+            if (lane == 0) mbar_arrive(&bar_p[x][b]);
+            const float2 both = add2(sum[0], sum[1]);
+            l += both.x + both.y;
         }
-        const int n = jt_hi[x] - jt_lo[x];
-        if (n > 0 && ok && !mbar_wait(&bar_pv[x], (n - 1) & 1, limit)) give_up();
+        if (n > 0 && ok) wait(&bar_o[x], 0);               // O is complete
         __syncwarp();
         tc_fence_after();
         if (lsplit == 0) {
@@ -490,11 +505,8 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
     __syncthreads();
     if (warp == 9) {
         tc_fence_after();
-        if (s_err) {                                       // products in flight end before their accumulators are given back
-            if (lane == 0) umma_commit(&bar_end);
-            __syncwarp();
-            mbar_wait(&bar_end, 0, limit);
-        }
+        if (s_err) mbar_wait(&bar_end, 0, limit);          // products in flight end before their accumulators are given back
+        __syncwarp();
         tmem_dealloc(tmem, 512);
     }
     if (tid == 0 && s_err) report_paged(a.hdr, 1);

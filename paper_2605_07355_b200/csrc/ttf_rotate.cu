@@ -36,21 +36,6 @@ template <int V> __device__ __forceinline__ void item_at(int it, int rot, int in
     e1 = halves ? rot / 2 + it * V : e0 + V;
 }
 
-// a * b + c and a * b on two channels at once (one instruction of the fp32 pipe)
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 d;
-    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
-        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return d;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    float2 d;
-    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
-        "mul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
-}
 // y[] = x[] * b[] (+ c[]) over N channels
 template <int N> __device__ __forceinline__ void vmul(float (&y)[N], const float (&x)[N], const float (&b)[N]) {
     if constexpr (N == 1) y[0] = x[0] * b[0];
