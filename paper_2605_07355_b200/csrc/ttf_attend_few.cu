@@ -62,7 +62,7 @@ k_attend_few(const __grid_constant__ FewMaps maps, const __grid_constant__ Atten
     pdl_wait();
     Tile t;
     // (every CTA of a cluster has the same tile, and so the same answer)
-    if (!find_tile(a, kMmaRows, 0, work / a.cache.heads, blockIdx.x == 0, t)) return;
+    if (!find_tile(a, Cut{Divisor{0, 0, 0}, 4}, work / a.cache.heads, blockIdx.x == 0, t)) return;
     if (lsplit) cluster_arrive();                          // (waited for before anything is sent to another rank)
     const SeqRange r = t.r;
     const int* const table = a.seq.table + (long long)t.seq * a.seq.table_stride;

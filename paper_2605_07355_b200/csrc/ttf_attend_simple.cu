@@ -53,7 +53,7 @@ k_attend_simple(const __grid_constant__ AttendArgs a, int lsplit)
     pdl_wait();
     Tile t;
     // (every CTA of a cluster has the same tile, and so the same answer)
-    if (!find_tile(a, kSimpleRows, 0, blockIdx.x >> lsplit, blockIdx.x == 0 && blockIdx.y == 0, t)) return;
+    if (!find_tile(a, Cut{Divisor{0, 0, 0}, 5}, blockIdx.x >> lsplit, blockIdx.x == 0 && blockIdx.y == 0, t)) return;
     const SeqRange r = t.r;
     const int* const table = a.seq.table + (long long)t.seq * a.seq.table_stride;
     const int row0 = t.tile * kSimpleRows;                 // first packed row

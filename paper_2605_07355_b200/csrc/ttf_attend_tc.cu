@@ -17,7 +17,7 @@
 // nothing is lost, since bf16 and fp32 keep their relative precision), which after the first blocks is rare.
 //
 // Few tiles over many slots: the CTAs of a cluster share the blocks, and each finishes a part of the rows from what all of them
-// leave in shared memory.
+// send into its shared memory.
 //
 // Masks: only blocks that some row of the tile does not see whole are masked, by selection, whatever the keys hold.  Values of
 // slots that no row of the CTA sees (stale rows of a page behind the length, slots before the window) are zeroed in shared memory.
@@ -45,12 +45,16 @@ template <int DP> struct AttendShape {
     static constexpr int TILE = HALVES * COL;                      // a Q tile, a ring slot
     static constexpr int RING = DP == 128 ? 5 : 8;
     static constexpr int SMEM = 2 * TILE + RING * TILE;
-    static constexpr int OP = DP + 4;                              // floats of a row that ranks exchange; behind both tiles'
-    static constexpr int ML = 2 * kAtRows * OP;                    // rows [maximum, sum][tile][row]
+    static constexpr int ML = 2 * kAtRows * DP;                    // what ranks send: [rank][tile][channel][row], then maxima, sums
     static constexpr uint32_t O_COL = 256;                         // tensor memory: S0 0, S1 128, O0, O1 from 256 on
 };
 
 struct AttendMaps { CUtensorMap q, k, v; };
+struct AttendCut {
+    Cut pair;                                      // the tokens of a CTA: two tiles
+    Divisor block, group;                          // slots of a block, heads of a group
+    int per_tile, box_rows, lsplit;                // tokens of a tile, rows of a TMA tile (a page or a part of one)
+};
 
 // D[tmem] (+)= A[tmem] . B[smem desc], issued by one thread
 __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, bool accumulate) {
@@ -121,21 +125,9 @@ __device__ __forceinline__ float exp2_approx(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ float ld_cluster_f32_(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-}
-
 template <int DP>
 __global__ void __launch_bounds__(kAtThreads, 1)
-k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ AttendArgs a, int lsplit, int per_tile, int block,
-            int box_rows)
+k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ AttendArgs a, const __grid_constant__ AttendCut cut)
 {
     using S = AttendShape<DP>;
     extern __shared__ unsigned char at_raw[];
@@ -144,15 +136,48 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
     __shared__ int s_err;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int lsplit = cut.lsplit, per_tile = cut.per_tile, block = (int)cut.block.d, box_rows = cut.box_rows;
     const int split = 1 << lsplit, rank = lsplit ? (int)cluster_rank() : 0;
     const int work = blockIdx.x >> lsplit;
     const int hk = work % a.cache.heads;
     const int limit = a.wait_limit;
 
+    // what does not depend on earlier work in the stream comes first
+    const uint32_t base_addr = (smem_u32(at_raw) + 1023u) & ~1023u;
+    unsigned char* const smem = at_raw + (base_addr - smem_u32(at_raw));
+    if (warp == 8) {
+        if (lane < S::RING) { mbar_init(&bar_full[lane], 1); mbar_init(&bar_empty[lane], 2); }
+        if (lane == 0) {
+            mbar_init(&bar_q, 1); mbar_init(&bar_raw, 1); mbar_init(&bar_end, 2);
+            for (int x = 0; x < 2; ++x) {
+                for (int b = 0; b < 2; ++b) { mbar_init(&bar_s[x][b], 1); mbar_init(&bar_p[x][b], 4); }
+                mbar_init(&bar_pv[x], 1); mbar_init(&bar_o[x], 1);
+            }
+            s_err = 0;
+            tensormap_prefetch(&maps.q); tensormap_prefetch(&maps.k); tensormap_prefetch(&maps.v);
+        }
+        mbar_init_fence();
+    }
+    // rows of the ring that no page fills (blocks of less than 128 slots): zero for good
+    if (block < kAtSlots) {
+        for (int col = 0; col < S::RING * S::HALVES; ++col)
+            for (int o = block * 8 + tid; o < kAtSlots * 8; o += kAtThreads)
+                *reinterpret_cast<uint4*>(smem + 2 * S::TILE + (size_t)col * S::COL + o * 16) = make_uint4(0, 0, 0, 0);
+        fence_async_smem();
+    }
+    if (warp == 9) tmem_alloc(&s_tmem, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+
     pdl_wait();
     Tile t;
     // (every CTA of a cluster has the same tile, and so the same answer)
-    if (!find_tile(a, 0, 2 * per_tile, work / a.cache.heads, blockIdx.x == 0, t)) return;
+    if (!find_tile(a, cut.pair, work / a.cache.heads, blockIdx.x == 0, t)) {
+        if (warp == 9) tmem_dealloc(tmem, 512);
+        return;
+    }
     const SeqRange r = t.r;
     const int tok0 = t.tile * 2 * per_tile;                // first token of the CTA
     int ntok[2];
@@ -162,7 +187,7 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
     // the blocks of this rank, and of each of its tiles
     const int tok_z = tok0 + ntok[0] + ntok[1] - 1;
     const int lo_u = seen_by(r, tok0, a.causal, a.window).lo, hi_u = seen_by(r, tok_z, a.causal, a.window).hi;
-    const int b_lo = lo_u / block, b_hi = hi_u > lo_u ? (hi_u + block - 1) / block : b_lo;
+    const int b_lo = quotient(lo_u, cut.block), b_hi = hi_u > lo_u ? quotient(hi_u + block - 1, cut.block) : b_lo;
     const int j_lo = b_lo + (int)((long long)(b_hi - b_lo) * rank >> lsplit);
     const int j_hi = b_lo + (int)((long long)(b_hi - b_lo) * (rank + 1) >> lsplit);
     int jt_lo[2], jt_hi[2];
@@ -170,35 +195,10 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
     for (int x = 0; x < 2; ++x) {
         const int ta = tok0 + x * per_tile;
         const int lo = seen_by(r, ta, a.causal, a.window).lo, hi = seen_by(r, ta + ntok[x] - 1, a.causal, a.window).hi;
-        jt_lo[x] = max(j_lo, lo / block);
-        jt_hi[x] = ntok[x] > 0 && hi > lo ? min(j_hi, (hi + block - 1) / block) : 0;
+        jt_lo[x] = max(j_lo, quotient(lo, cut.block));
+        jt_hi[x] = ntok[x] > 0 && hi > lo ? min(j_hi, quotient(hi + block - 1, cut.block)) : 0;
         if (jt_hi[x] < jt_lo[x]) jt_hi[x] = jt_lo[x];
     }
-
-    const uint32_t base_addr = (smem_u32(at_raw) + 1023u) & ~1023u;
-    unsigned char* const smem = at_raw + (base_addr - smem_u32(at_raw));
-    if (tid == 0) {
-        mbar_init(&bar_q, 1); mbar_init(&bar_raw, 1); mbar_init(&bar_end, 2);
-        for (int s = 0; s < S::RING; ++s) { mbar_init(&bar_full[s], 1); mbar_init(&bar_empty[s], 2); }
-        for (int x = 0; x < 2; ++x) { for (int b = 0; b < 2; ++b) { mbar_init(&bar_s[x][b], 1); mbar_init(&bar_p[x][b], 4); } mbar_init(&bar_pv[x], 1); mbar_init(&bar_o[x], 1); }
-        mbar_init_fence();
-        s_err = 0;
-        tensormap_prefetch(&maps.q); tensormap_prefetch(&maps.k); tensormap_prefetch(&maps.v);
-    }
-    // rows of the ring that no page fills (blocks of less than 128 slots): zero for good
-    if (block < kAtSlots) {
-        const int n = (kAtSlots - block) * 8;              // 16-byte pieces of a column
-        for (int i = tid; i < n * S::RING * S::HALVES; i += kAtThreads) {
-            const int col = i / n, o = i - col * n;
-            *reinterpret_cast<uint4*>(smem + 2 * S::TILE + (size_t)col * S::COL + block * 128 + o * 16) = make_uint4(0, 0, 0, 0);
-        }
-        fence_async_smem();
-    }
-    if (warp == 9) tmem_alloc(&s_tmem, 512);
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    const uint32_t tmem = s_tmem;
     auto failed = [&]() { return *(volatile int*)&s_err != 0; };
     auto give_up = [&]() { atomicExch(&s_err, 1); };
     // (a role that gives up is noticed by the others, or their own waits run out)
@@ -257,9 +257,11 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
                     ok = __all_sync(0xffffffffu, wait(&bar_raw, raw & 1));
                     if (!ok) break;
                     ++raw;
-                    for (int i = lane; i < block * 8 * S::HALVES; i += 32) {
-                        const int h = i / (block * 8), o = i - h * (block * 8), at = s0 + (o >> 3);
-                        if (at < lo_u || at >= hi_u) *reinterpret_cast<uint4*>(to + h * S::COL + o * 16) = make_uint4(0, 0, 0, 0);
+                    const int head = max(0, lo_u - s0) * 8, tail = max(0, hi_u - s0) * 8;      // in 16-byte pieces
+#pragma unroll
+                    for (int h = 0; h < S::HALVES; ++h) {
+                        for (int o = lane; o < head; o += 32) *reinterpret_cast<uint4*>(to + h * S::COL + o * 16) = make_uint4(0, 0, 0, 0);
+                        for (int o = tail + lane; o < block * 8; o += 32) *reinterpret_cast<uint4*>(to + h * S::COL + o * 16) = make_uint4(0, 0, 0, 0);
                     }
                     fence_async_smem();
                     __syncwarp();
@@ -340,7 +342,7 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t s_at = lanes + x * 128, o_at = lanes + S::O_COL + x * DP;
         const int nrow = ntok[x] * a.group;
-        const Seen mine = row < nrow ? seen_by(r, tok0 + x * per_tile + row / a.group, a.causal, a.window) : Seen{0, 0};
+        const Seen mine = row < nrow ? seen_by(r, tok0 + x * per_tile + quotient(row, cut.group), a.causal, a.window) : Seen{0, 0};
         // slots that every row of the tile sees
         const int all_lo = ntok[x] > 0 ? seen_by(r, tok0 + x * per_tile + ntok[x] - 1, a.causal, a.window).lo : 0;
         const int all_hi = ntok[x] > 0 ? seen_by(r, tok0 + x * per_tile, a.causal, a.window).hi : 0;
@@ -409,49 +411,64 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
             l += both.x + both.y;
         }
         if (n > 0 && ok) wait(&bar_o[x], 0);               // O is complete
+        if (n == 0 && j_lo < j_hi) wait(&bar_q, 0);        // (rows go out through the place of Q, which may still be on its way)
         __syncwarp();
         tc_fence_after();
         if (lsplit == 0) {
-            if (row < nrow || n > 0) {                     // (whole warps take part in the loads from tensor memory)
-                const float inv = l == 0.f ? 0.f : 1.f / l;
-                const int token = tok0 + x * per_tile + (row < nrow ? row / a.group : 0);
-                const int head = hk * a.group + (row < nrow ? row % a.group : 0);
-                uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<bf16_t*>(a.out.data) + (long long)(r.first + token) * a.out.row + (long long)head * a.out.head);
-                const bool on = row < nrow && in_bounds(a.hdr, 8, (long long)r.first + token, a.seq.rows);
-#pragma unroll 1
-                for (int i = 0; i < DP; i += 32) {
-                    uint32_t o[32];
-                    if (n > 0) { tmem_ld32(o_at + i, o); tmem_ld_wait(o); }
+            // rows go out through the tile's own Q in shared memory (nobody reads it any more), so that a row leaves as a whole:
+            // 16-byte piece q of row i lies at piece q ^ (i & 7)
+            constexpr int PIECES = DP / 8;
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            unsigned char* const stage = smem + x * S::TILE + (warp & 3) * 32 * PIECES * 16;
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        uint4 w = make_uint4(0, 0, 0, 0);
-                        if (n > 0 && l != 0.f) {
-                            w.x = bf16_pair(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
-                            w.y = bf16_pair(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
-                            w.z = bf16_pair(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
-                            w.w = bf16_pair(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
-                        }
-                        if (on && i + e < a.cache.dim) dst[(i + e) / 8] = w;
+            for (int i = 0; i < DP; i += 64) {
+                uint32_t o[64];
+                if (n > 0) { tmem_ld32(o_at + i, o); tmem_ld32(o_at + i + 32, o + 32); tmem_ld_wait(o); }
+#pragma unroll
+                for (int e = 0; e < 64; e += 8) {
+                    uint4 w = make_uint4(0, 0, 0, 0);
+                    if (n > 0 && l != 0.f) {
+                        w.x = bf16_pair(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
+                        w.y = bf16_pair(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
+                        w.z = bf16_pair(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
+                        w.w = bf16_pair(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
                     }
+                    *reinterpret_cast<uint4*>(stage + (lane * PIECES + (((i + e) / 8) ^ (lane & 7))) * 16) = w;
                 }
             }
+            __syncwarp();
+            constexpr int ROWS = 32 / PIECES;              // rows at a time
+            const int q = lane % PIECES;
+            const bool on = q * 8 < a.cache.dim;
+#pragma unroll 4
+            for (int i = lane / PIECES; i < 32; i += ROWS) {
+                const int at = (warp & 3) * 32 + i;
+                const int token = quotient(at, cut.group), head = hk * a.group + at - token * a.group;
+                const long long to = r.first + tok0 + x * per_tile + token;
+                const uint4 w = *reinterpret_cast<const uint4*>(stage + (i * PIECES + (q ^ (i & 7))) * 16);
+                if (on && at < nrow && in_bounds(a.hdr, 8, to, a.seq.rows))
+                    *reinterpret_cast<uint4*>(reinterpret_cast<bf16_t*>(a.out.data) + to * a.out.row + (long long)head * a.out.head + q * 8) = w;
+            }
         } else {
-            // the other tile's products may still read the ring: what is exchanged goes where Q and the ring were, so both
-            // tiles have to be through
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            float* const ml = reinterpret_cast<float*>(smem) + S::ML + x * kAtRows + row;
-            ml[0] = m; ml[2 * kAtRows] = l;
-            float* const mine_o = reinterpret_cast<float*>(smem) + (x * kAtRows + row) * S::OP;
+            // Every rank finishes 1 / split of the rows of both tiles: when all of them are through with their shared memory, rank p's
+            // rows p * each .. + each - 1 are sent there from all ranks, channel by channel, so that the lanes of a warp write
+            // consecutive words (16 bytes of a row per lane travel as 32 packets: 10000 cycles for 128 KB).
+            const int each = kAtRows >> lsplit, to = row >> (7 - lsplit), col = row & (each - 1);
+            __syncwarp();
+            cluster_arrive();
+            cluster_wait();
+            const uint32_t ml = cluster_addr(base_addr + (uint32_t)(S::ML + (rank * 2 + x) * each + col) * 4, to);
+            st_cluster_f32(ml, m);
+            st_cluster_f32(ml + 2 * kAtRows * 4, l);
             if (n > 0) {
-#pragma unroll 1
+                const uint32_t at = cluster_addr(base_addr + (uint32_t)((rank * 2 + x) * DP * each + col) * 4, to);
+#pragma unroll
                 for (int i = 0; i < DP; i += 32) {
                     uint32_t o[32];
                     tmem_ld32(o_at + i, o);
                     tmem_ld_wait(o);
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<float4*>(mine_o + i + e) = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]),
-                                                                                  __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
+                    for (int e = 0; e < 32; ++e) st_cluster_u32(at + (uint32_t)((i + e) * each * 4), o[e]);
                 }
             }
         }
@@ -460,46 +477,40 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
 
     if (lsplit) {
         __syncwarp();
+        if (warp >= 8) { cluster_arrive(); cluster_wait(); }               // (the softmax warps were there before they sent)
         cluster_arrive();
         cluster_wait();
-        // rows row % split == rank of both tiles: first every rank's maxima and sums, then four channels per thread
-        constexpr int Q4 = DP / 4;
-        const int mine = 2 * (kAtRows >> lsplit);          // row i of them: tile i & 1, row (i >> 1) * split + rank
-        float* const s_f = reinterpret_cast<float*>(smem) + S::ML + 4 * kAtRows;              // [i][rank]: maxima, then sums
-        for (int e = tid; e < mine << lsplit; e += kAtThreads) {
-            const int p = e & (split - 1), i = e >> lsplit, at = S::ML + (i & 1) * kAtRows + ((i >> 1) << lsplit) + rank;
-            s_f[e] = ld_cluster_f32_(cluster_addr(base_addr + (uint32_t)at * 4, p));
-            s_f[2 * kAtRows + e] = ld_cluster_f32_(cluster_addr(base_addr + (uint32_t)(at + 2 * kAtRows) * 4, p));
-        }
-        __syncthreads();
-        for (int e = tid; e < mine * Q4; e += kAtThreads) {
-            const int i = e / Q4, d = (e - i * Q4) * 4, x = i & 1, row = ((i >> 1) << lsplit) + rank;
+        const int each = kAtRows >> lsplit, rows2 = 2 * each;
+        const float* const f = reinterpret_cast<const float*>(smem);
+        for (int e = tid; e < rows2 * (DP / 8); e += kAtThreads) {
+            const int i = e & (rows2 - 1), d = (e >> (8 - lsplit)) * 8;   // row i of the rank's: tile i / each
+            const int x = i >= each, col = i - x * each, row = rank * each + col;
             if (row >= ntok[x] * a.group || d >= a.cache.dim) continue;
-            const uint32_t at_o = base_addr + (uint32_t)((x * kAtRows + row) * S::OP + d) * 4;
-            const float* const fm = s_f + (i << lsplit);
-            float m = -INFINITY;
-            for (int p = 0; p < split; ++p) m = fmaxf(m, fm[p]);
-            const float ref = m == -INFINITY ? 0.f : m;
-            float l = 0.f;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            float mx = -INFINITY;
 #pragma unroll 4
+            for (int p = 0; p < split; ++p) mx = fmaxf(mx, f[S::ML + p * rows2 + i]);
+            const float ref = mx == -INFINITY ? 0.f : mx;
+            float l = 0.f, o[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) o[c] = 0.f;
+#pragma unroll 2
             for (int p = 0; p < split; ++p) {
-                const float4 v = ld_cluster_f32x4(cluster_addr(at_o, p));
-                const float lp = fm[2 * kAtRows + p], f = exp2_approx(fm[p] - ref);
+                const float lp = f[S::ML + 2 * kAtRows + p * rows2 + i], w = exp2_approx(f[S::ML + p * rows2 + i] - ref);
                 if (lp == 0.f) continue;                   // that rank saw nothing of the row
-                l = fmaf(f, lp, l);
-                o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+                const float* const v = f + (p * 2 + x) * DP * each + d * each + col;
+                l = fmaf(w, lp, l);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) o[c] = fmaf(w, v[c * each], o[c]);
             }
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            const int token = tok0 + x * per_tile + row / a.group, head = hk * a.group + row % a.group;
-            uint2 w = make_uint2(0, 0);
-            if (l != 0.f) w = make_uint2(bf16_pair(o.x * inv, o.y * inv), bf16_pair(o.z * inv, o.w * inv));
+            const int in_tile = quotient(row, cut.group), token = tok0 + x * per_tile + in_tile, head = hk * a.group + row - in_tile * a.group;
+            uint4 w = make_uint4(0, 0, 0, 0);
+            if (l != 0.f)
+                w = make_uint4(bf16_pair(o[0] * inv, o[1] * inv), bf16_pair(o[2] * inv, o[3] * inv), bf16_pair(o[4] * inv, o[5] * inv),
+                               bf16_pair(o[6] * inv, o[7] * inv));
             if (in_bounds(a.hdr, 8, (long long)r.first + token, a.seq.rows))
-                *reinterpret_cast<uint2*>(reinterpret_cast<bf16_t*>(a.out.data) + (long long)(r.first + token) * a.out.row + (long long)head * a.out.head + d) = w;
+                *reinterpret_cast<uint4*>(reinterpret_cast<bf16_t*>(a.out.data) + (long long)(r.first + token) * a.out.row + (long long)head * a.out.head + d) = w;
         }
-        __syncwarp();
-        cluster_arrive();                                  // nobody leaves while its sums may be read
-        cluster_wait();
     }
     tc_fence_before();
     __syncthreads();
@@ -565,8 +576,15 @@ template <int DP> static cudaError_t launch_tc_t(const AttendArgs& a, cudaStream
     const long long ctas = most_tiles(a, 0, 2 * per) * a.cache.heads;
     const long long slots = (long long)a.seq.table_pages * page;
     const long long reach = (long long)a.window + a.seq.rows, longest = a.window > 0 && reach < slots ? reach : slots;
+    // CTAs (a power of two) that share the slots of a pair of tiles.  A join costs 8 to 11 us (distributed shared memory takes in
+    // some 14 bytes per clock, and the partial rows are 128 KB), a block of 128 slots 1.9 us.  Where the CTAs do not fill the SMs
+    // shares go down to 512 slots (65 rows over 4000 slots, 8 key heads: 71 us alone, 49 / 33 shared by 2 / 8; over 1024 slots 23.2
+    // and 25.4 / 21.8); where they do, two share sequences of more than 8192 slots, whose CTAs would be long against the call (6
+    // sequences of 60 - 900 new rows over 400 - 12000, 2 key heads: 188 / 103 / 127 us with 1 / 2 / 4; 4096 new rows over 16384, 8 key
+    // heads: 937 / 891 / 1108; 2760 new rows alone 84 / 133 / 227).
     int ls = 0;
-    while (ls < 3 && (ctas << (ls + 1)) <= sm_count() && (longest >> (ls + 1)) >= 2 * kAtSlots) ++ls;
+    while (ls < 3 && (ctas << (ls + 1)) <= sm_count() && longest >= 2048 && (longest >> (ls + 1)) >= 512) ++ls;
+    if (ls == 0 && longest >= 8192) ls = 1;
     if ((ctas << ls) > 0x7fffffffLL) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(ctas << ls)); cfg.blockDim = dim3(kAtThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
@@ -576,7 +594,8 @@ template <int DP> static cudaError_t launch_tc_t(const AttendArgs& a, cudaStream
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = 1u << ls; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = ls ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, k_attend_tc<DP>, maps, a, ls, per, block, box);
+    AttendCut cut = {cut_tokens(2 * per), make_divisor(block), make_divisor(a.group), per, box, ls};
+    return cudaLaunchKernelEx(&cfg, k_attend_tc<DP>, maps, a, cut);
 }
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t st) {
     return a.cache.dim <= 64 ? launch_tc_t<64>(a, st) : launch_tc_t<128>(a, st);

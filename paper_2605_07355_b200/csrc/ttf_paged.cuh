@@ -198,14 +198,18 @@ __device__ __forceinline__ Seen seen_by(const SeqRange& r, int token, int causal
 }
 
 // The tile of this CTA.  The new rows of a sequence times the query heads of a group are packed rows (row = token * group +
-// head), cut into tiles of `per` tokens (tokens > 0) or of `rows` packed rows; tiles are numbered over the sequences, and
+// head), cut into tiles of so many tokens or of so many packed rows; tiles are numbered over the sequences, and
 // tile `index` from the end is looked up (with a causal mask the last tiles of a sequence take longest: they come first).
 // Every warp does it for itself.  False: there is no such tile.
 struct Tile { int seq, tile; SeqRange r; };
-__device__ __forceinline__ int tiles_of(int n, int group, int rows, int per) {
-    return per > 0 ? (n + per - 1) / per : (int)(((long long)n * group + rows - 1) / rows);
+struct Cut { Divisor tokens; int lrows; };         // tiles of `tokens` tokens, or (tokens.d = 0) of 2^lrows packed rows
+inline Cut cut_tokens(int per) { return Cut{make_divisor(per), 0}; }
+inline Cut cut_rows(int lrows) { return Cut{Divisor{0, 0, 0}, lrows}; }
+__device__ __forceinline__ int tiles_of(int n, int group, const Cut& cut) {
+    return cut.tokens.d ? quotient(n + (int)cut.tokens.d - 1, cut.tokens)
+                        : (int)(((long long)n * group + (1 << cut.lrows) - 1) >> cut.lrows);
 }
-__device__ __forceinline__ bool find_tile(const AttendArgs& a, int rows, int per, int index, bool report, Tile& t) {
+__device__ __forceinline__ bool find_tile(const AttendArgs& a, const Cut& cut, int index, bool report, Tile& t) {
     const int lane = threadIdx.x & 31;
     int total = 0, c = 0;
     bool bad = false;
@@ -215,7 +219,7 @@ __device__ __forceinline__ bool find_tile(const AttendArgs& a, int rows, int per
         if (s0 + lane < a.seq.seqs) {
             r = seq_range(a.seq, s0 + lane, a.cache.page);
             bad |= !r.ok;
-            c = tiles_of(r.n, a.group, rows, per);
+            c = tiles_of(r.n, a.group, cut);
         }
         total += __reduce_add_sync(0xffffffffu, c);
     }
@@ -227,7 +231,7 @@ __device__ __forceinline__ bool find_tile(const AttendArgs& a, int rows, int per
             c = 0;
             if (s0 + lane < a.seq.seqs) {
                 r = seq_range(a.seq, s0 + lane, a.cache.page);
-                c = tiles_of(r.n, a.group, rows, per);
+                c = tiles_of(r.n, a.group, cut);
             }
         }
         int upto = c;                              // inclusive scan
