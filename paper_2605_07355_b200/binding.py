@@ -179,6 +179,8 @@ def _marshal():
         except ImportError as e:
             raise FileNotFoundError("_marshal.so not found: build it with `python -m paper_2605_07355_b200.build`") from e
         m.bind(*[ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in _FAST_FUNCTIONS])
+        if _current_device is not None and _current_raw_stream is not None:
+            m.bind_torch(torch.float32, torch.bfloat16, torch.int32, _current_device, _current_raw_stream)
         _fast = m
     return _fast
 
@@ -673,6 +675,13 @@ def ttf_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: 
     """ttf_rotate: norm (where there is a weight) and rotation of the heads of q and k [rows, heads, channels] (either may be
     None) by positions int32 [rows] or [rows, axes]; freq float32 [rot_dim / 2].  Only the first `count` rows (int32[1] on the
     device; None: all) are read and written.  Returns (out_q, out_k); out_q may be q itself.  Does not synchronise."""
+    if (q is None or out_q is not None) and (k is None or out_k is not None):        # nothing to allocate: the plain case
+        rc = (_fast or _marshal()).rotate_tensors(q, k, positions, freq, q_weight, k_weight, rot_dim, interleaved, sections,
+                                                  cyclic, factor, eps, count, out_q, out_k, stream)
+        if rc == TTF_OK:
+            return out_q, out_k
+        if rc > 0:
+            raise TTFError(rc, "ttf_rotate")
     like = q if q is not None else k
     if like is None:
         raise ValueError("q or k must be given")
@@ -740,6 +749,14 @@ def ttf_cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_
     strides with contiguous channels).  Rows start[b] .. start[b + 1] - 1 are the last ones of the length[b] tokens of
     sequence b; slot s lies in page table[b, s // page_size] (all int32 on the device).  With q the queries are normed and
     rotated by the same kernel; returns out_q (None without q).  Does not synchronise."""
+    if q is None or out_q is not None:                     # nothing to allocate: the plain case
+        rc = (_fast or _marshal()).cache_append_tensors(k, v, k_cache, v_cache, start, length, table, positions, freq, q_weight,
+                                                        k_weight, rot_dim, interleaved, sections, cyclic, factor, eps, q, out_q,
+                                                        stream)
+        if rc == TTF_OK:
+            return out_q
+        if rc > 0:
+            raise TTFError(rc, "ttf_cache_append")
     if not k.is_cuda:
         raise ValueError(f"k must be a CUDA tensor, got one on {k.device}")
     there = _elsewhere(k)
@@ -777,6 +794,12 @@ def ttf_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, st
     """ttf_attend: attention of the new rows q [rows, heads, channels] over their sequences' slots of the cache, as
     ttf_cache_append has left it (same start, length and table).  causal: a row sees the slots up to its own; window > 0: of
     these only the last `window`.  Rows behind start[-1] are left as they are.  Returns out.  Does not synchronise."""
+    if out is not None:                                    # nothing to allocate: the plain case
+        rc = (_fast or _marshal()).attend_tensors(q, k_cache, v_cache, start, length, table, scale, causal, window, out, stream)
+        if rc == TTF_OK:
+            return out
+        if rc > 0:
+            raise TTFError(rc, "ttf_attend")
     if not q.is_cuda:
         raise ValueError(f"q must be a CUDA tensor, got one on {q.device}")
     there = _elsewhere(q)

@@ -1,7 +1,8 @@
 /* Argument marshalling of the Python binding in C: the entry points of include/ttf.h that a program calls per clip or
  * per batch.  A call through ctypes converts its 12 to 17 arguments one by one in about 4 us, which is more than the
- * driver takes to launch a kernel; here it is about 0.3 us.  No CUDA, no torch: pointers and streams arrive as integers
- * (0 = NULL), the addresses of the library's functions are handed in once by bind().  The GIL is released around every
+ * driver takes to launch a kernel; here it is about 0.3 us.  No CUDA and no torch headers: pointers and streams arrive as integers
+ * (0 = NULL), or tensors are asked for their attributes as Python would; the addresses of the library's functions are handed
+ * in once by bind().  The GIL is released around every
  * call. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -273,10 +274,188 @@ static PyObject* m_attend(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     CALL(fn.attend(given(&q), &sq, &c, scale, causal, window, given(&o), st));
 }
 
+/* ---- tensors as they are -------------------------------------------------------------------------------------------
+ * ttf_rotate, ttf_cache_append and ttf_attend take seven to twelve tensors each; asking every one for its shape, strides,
+ * address, type and device from Python costs more than the kernels of a small call take.  These functions ask here (about
+ * 0.3 us per tensor), and answer -1 where anything is not exactly as the plain case has it: the Python code then looks at
+ * the arguments one by one, raises what is to be raised, or makes the call itself.  Nothing is kept between calls. */
+static PyObject *t_f32, *t_bf16, *t_i32;                   /* the torch.dtype objects */
+static PyObject *f_device, *f_stream;                      /* current device; current raw stream of a device */
+static PyObject *s_shape, *s_dtype, *s_stride, *s_ptr, *s_dev;
+
+typedef struct { long long n[4], s[4]; int dims, dev, type; void* p; } Facts;      /* type: 0 fp32, 1 bf16, 2 int32 */
+
+static int longs(PyObject* t, long long* to) {             /* a tuple of up to four ints; its length, or -1 */
+    if (!t || !PyTuple_Check(t) || PyTuple_GET_SIZE(t) > 4) { Py_XDECREF(t); return -1; }
+    int n = (int)PyTuple_GET_SIZE(t);
+    for (int i = 0; i < n; ++i) to[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(t, i));
+    Py_DECREF(t);
+    return n;
+}
+static int facts(PyObject* x, Facts* f) {
+    PyObject* o;
+    f->dims = longs(PyObject_GetAttr(x, s_shape), f->n);
+    if (f->dims < 0) return 0;
+    if (longs(PyObject_CallMethodNoArgs(x, s_stride), f->s) != f->dims) return 0;
+    if (!(o = PyObject_GetAttr(x, s_dtype))) return 0;
+    f->type = o == t_f32 ? 0 : (o == t_bf16 ? 1 : (o == t_i32 ? 2 : -1));
+    Py_DECREF(o);
+    if (!(o = PyObject_CallMethodNoArgs(x, s_dev))) return 0;
+    f->dev = (int)PyLong_AsLong(o);
+    Py_DECREF(o);
+    if (!(o = PyObject_CallMethodNoArgs(x, s_ptr))) return 0;
+    f->p = PyLong_AsVoidPtr(o);
+    Py_DECREF(o);
+    return f->type >= 0 && !PyErr_Occurred();
+}
+/* [rows, heads, channels] of the type and device of `like` (rows and channels of it too) */
+static int heads_of(PyObject* x, const Facts* like, ttf_heads* h) {
+    Facts f;
+    h->data = NULL; h->heads = 0; h->row_stride = h->head_stride = 0;
+    if (x == Py_None) return 1;
+    if (!facts(x, &f) || f.dims != 3 || f.type != like->type || f.dev != like->dev || f.n[0] != like->n[0] || f.n[2] != like->n[2] ||
+        (f.s[2] != 1 && f.n[2] > 1) || f.n[1] < 1 || f.n[1] > 0x7fffffff || !f.p) return 0;
+    h->data = f.p; h->row_stride = f.s[0]; h->head_stride = f.s[1]; h->heads = (int)f.n[1];
+    return 1;
+}
+/* one contiguous axis of `n` elements (n < 0: any number) */
+static int line_of(PyObject* x, int type, int dev, long long n, const void** p, long long* got) {
+    Facts f;
+    if (!facts(x, &f) || f.dims != 1 || f.type != type || f.dev != dev || (n >= 0 && f.n[0] != n) || (f.n[0] > 1 && f.s[0] != 1)) return 0;
+    *p = f.p;
+    if (got) *got = f.n[0];
+    return 1;
+}
+static int cache_of(PyObject* k, PyObject* v, const Facts* like, ttf_cache* c) {
+    Facts a, b;
+    if (!facts(k, &a) || !facts(v, &b) || a.dims != 4 || b.dims != 4 || a.type != like->type || b.type != like->type ||
+        a.dev != like->dev || b.dev != like->dev || a.n[3] != like->n[2]) return 0;
+    for (int i = 0; i < 4; ++i) if (a.n[i] != b.n[i] || a.n[i] < 1 || a.n[i] > 0x7fffffff) return 0;
+    if ((a.s[3] != 1 || b.s[3] != 1) && a.n[3] > 1) return 0;
+    c->k = a.p; c->k_page = a.s[0]; c->k_row = a.s[1]; c->k_head = a.s[2];
+    c->v = b.p; c->v_page = b.s[0]; c->v_row = b.s[1]; c->v_head = b.s[2];
+    c->pages = (int)a.n[0]; c->page_size = (int)a.n[1]; c->heads = (int)a.n[2]; c->head_dim = (int)a.n[3]; c->dtype = a.type;
+    return 1;
+}
+static int sequences_of(PyObject* start, PyObject* length, PyObject* table, const Facts* like, ttf_sequences* q) {
+    Facts t;
+    if (!facts(table, &t) || t.dims != 2 || t.type != 2 || t.dev != like->dev || t.n[0] < 1 || t.n[1] < 1 || t.n[0] > 0x7ffffffe ||
+        t.n[1] > 0x7fffffff || (t.n[1] > 1 && t.s[1] != 1)) return 0;
+    if (!line_of(start, 2, like->dev, t.n[0] + 1, (const void**)&q->start, NULL) ||
+        !line_of(length, 2, like->dev, t.n[0], (const void**)&q->length, NULL)) return 0;
+    q->table = t.p; q->table_stride = t.n[0] > 1 ? t.s[0] : t.n[1]; q->table_pages = (int)t.n[1]; q->seqs = (int)t.n[0];
+    q->rows = (int)like->n[0];
+    return 1;
+}
+/* positions, freq, q_weight, k_weight, rot_dim, interleaved, sections, cyclic, factor, eps from a[0] on */
+static int rotation_of(PyObject* const* a, const Facts* like, ttf_rotation* r, const int** pos) {
+    Facts f;
+    if (!facts(a[0], &f) || f.type != 2 || f.dev != like->dev || f.dims < 1 || f.dims > 2 || f.n[0] != like->n[0]) return 0;
+    if (f.dims == 1) { f.n[1] = 1; f.s[1] = 1; }
+    if (f.n[1] < 1 || f.n[1] > 3 || (f.n[1] > 1 && f.s[1] != 1) || (f.n[0] > 1 && f.s[0] != f.n[1])) return 0;
+    *pos = f.p;
+    r->axes = (int)f.n[1];
+    long long rot = a[4] == Py_None ? like->n[2] : PyLong_AsLongLong(a[4]);
+    if (rot < 0 || rot > 0x7fffffff || !line_of(a[1], 0, like->dev, rot / 2, (const void**)&r->freq, NULL)) return 0;
+    r->rot_dim = (int)rot;
+    r->q_weight = r->k_weight = NULL;
+    if (a[2] != Py_None && !line_of(a[2], like->type, like->dev, like->n[2], &r->q_weight, NULL)) return 0;
+    if (a[3] != Py_None && !line_of(a[3], like->type, like->dev, like->n[2], &r->k_weight, NULL)) return 0;
+    r->interleaved = PyObject_IsTrue(a[5]);
+    r->section[0] = r->section[1] = r->section[2] = 0;
+    if (a[6] == Py_None) {
+        if (r->axes != 1) return 0;
+    } else {
+        if (!PyTuple_Check(a[6]) || PyTuple_GET_SIZE(a[6]) != r->axes) return 0;
+        for (int i = 0; i < r->axes; ++i) r->section[i] = (int)PyLong_AsLong(PyTuple_GET_ITEM(a[6], i));
+    }
+    r->cyclic = PyObject_IsTrue(a[7]);
+    r->factor = (float)PyFloat_AsDouble(a[8]);
+    r->eps = (float)PyFloat_AsDouble(a[9]);
+    return !PyErr_Occurred();
+}
+/* the first tensor decides type and device; that device has to be the current one.  Its current stream, or the one given */
+static int lead(PyObject* x, PyObject* stream, Facts* f, ttf_stream_t* st) {
+    if (!facts(x, f) || f->dims != 3 || f->type > 1 || f->dev < 0 || f->n[0] < 1 || f->n[0] > 0x7fffffff || f->n[2] < 1 || f->n[2] > 0x7fffffff) return 0;
+    PyObject* o = PyObject_CallNoArgs(f_device);
+    if (!o) return 0;
+    const long dev = PyLong_AsLong(o);
+    if (dev != f->dev) { Py_DECREF(o); return 0; }
+    if (stream == Py_None) {
+        PyObject* p = PyObject_CallOneArg(f_stream, o);
+        Py_DECREF(o);
+        if (!p) return 0;
+        *st = PyLong_AsVoidPtr(p);
+        Py_DECREF(p);
+    } else {
+        Py_DECREF(o);
+        if (!PyLong_Check(stream)) return 0;
+        *st = PyLong_AsVoidPtr(stream);
+    }
+    return !PyErr_Occurred();
+}
+#define UNUSUAL() do { PyErr_Clear(); return PyLong_FromLong(-1); } while (0)
+#define MADE(expr) do { int rc; Py_BEGIN_ALLOW_THREADS rc = (expr); Py_END_ALLOW_THREADS return PyLong_FromLong(rc); } while (0)
+
+/* f32, bf16, int32 (torch.dtype objects), current device, current raw stream */
+static PyObject* m_bind_torch(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    if (n != 5) { PyErr_SetString(PyExc_TypeError, "bind_torch() takes three types and two functions"); return NULL; }
+    for (int i = 0; i < 5; ++i) Py_INCREF(a[i]);
+    t_f32 = a[0]; t_bf16 = a[1]; t_i32 = a[2]; f_device = a[3]; f_stream = a[4];
+    s_shape = PyUnicode_InternFromString("shape"); s_dtype = PyUnicode_InternFromString("dtype");
+    s_stride = PyUnicode_InternFromString("stride"); s_ptr = PyUnicode_InternFromString("data_ptr");
+    s_dev = PyUnicode_InternFromString("get_device");
+    Py_RETURN_NONE;
+}
+/* q, k, the ten of rotation_of, count, out_q, out_k, stream */
+static PyObject* m_rotate_tensors(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    Facts like;
+    ttf_heads q, k, oq, ok;
+    ttf_rotation r;
+    ttf_stream_t st;
+    const int* pos;
+    const void* cnt = NULL;
+    if (n != 16 || !t_f32 || !lead(a[0] != Py_None ? a[0] : a[1], a[15], &like, &st) || !heads_of(a[0], &like, &q) ||
+        !heads_of(a[1], &like, &k) || !heads_of(a[13], &like, &oq) || !heads_of(a[14], &like, &ok) || q.heads != oq.heads ||
+        k.heads != ok.heads || !rotation_of(a + 2, &like, &r, &pos) ||
+        (a[12] != Py_None && !line_of(a[12], 2, like.dev, 1, &cnt, NULL))) UNUSUAL();
+    MADE(fn.rotate(given(&q), given(&k), (int)like.n[2], like.type, (int)like.n[0], cnt, pos, &r, given(&oq), given(&ok), st));
+}
+/* k, v, k_cache, v_cache, start, length, table, the ten of rotation_of, q, out_q, stream */
+static PyObject* m_cache_append_tensors(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    Facts like;
+    ttf_heads k, v, q, oq;
+    ttf_cache c;
+    ttf_sequences sq;
+    ttf_rotation r;
+    ttf_stream_t st;
+    const int* pos;
+    if (n != 20 || !t_f32 || !lead(a[0], a[19], &like, &st) || !heads_of(a[0], &like, &k) || !heads_of(a[1], &like, &v) ||
+        !heads_of(a[17], &like, &q) || !heads_of(a[18], &like, &oq) || q.heads != oq.heads || a[7] == Py_None ||
+        !cache_of(a[2], a[3], &like, &c) || !sequences_of(a[4], a[5], a[6], &like, &sq) || !rotation_of(a + 7, &like, &r, &pos)) UNUSUAL();
+    MADE(fn.cache_append(given(&k), given(&v), given(&q), pos, &r, &sq, &c, given(&oq), st));
+}
+/* q, k_cache, v_cache, start, length, table, scale, causal, window, out, stream */
+static PyObject* m_attend_tensors(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    Facts like;
+    ttf_heads q, o;
+    ttf_cache c;
+    ttf_sequences sq;
+    ttf_stream_t st;
+    if (n != 11 || !t_f32 || !lead(a[0], a[10], &like, &st) || !heads_of(a[0], &like, &q) || !heads_of(a[9], &like, &o) ||
+        q.heads != o.heads || !cache_of(a[1], a[2], &like, &c) || !sequences_of(a[3], a[4], a[5], &like, &sq)) UNUSUAL();
+    const double scale = PyFloat_AsDouble(a[6]);
+    const int causal = PyObject_IsTrue(a[7]);
+    const long window = PyLong_AsLong(a[8]);
+    if (PyErr_Occurred() || window != (int)window) UNUSUAL();
+    MADE(fn.attend(&q, &sq, &c, (float)scale, causal, (int)window, &o, st));
+}
+
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))m_##name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(bind), METHOD(compress), METHOD(compress_ws), METHOD(compress_segment),
                                 METHOD(compress_batch), METHOD(query), METHOD(query_ws), METHOD(restore), METHOD(stats),
                                 METHOD(rotate), METHOD(cache_append), METHOD(attend),
+                                METHOD(bind_torch), METHOD(rotate_tensors), METHOD(cache_append_tensors), METHOD(attend_tensors),
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__marshal(void) { return PyModule_Create(&module); }
