@@ -223,17 +223,25 @@ k_attend_simple(const __grid_constant__ AttendArgs a, int lsplit)
                 }
             }
         } else {
+            // (a slot outside a row's range is left out, not multiplied by zero: it may hold anything)
+            const int jz = max(z0, z1);
+#pragma unroll 4
+            for (int j = min(a0, a1); j < jz; ++j) {
+                const float p0 = ss[ty * 33 + j], p1 = ss[(ty + 16) * 33 + j];
+                const bool in0 = j >= a0 && j < z0, in1 = j >= a1 && j < z1;
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                for (int j = i ? a1 : a0; j < (i ? z1 : z0); ++j) {
-                    const float p = ss[(ty + 16 * i) * 33 + j];
-#pragma unroll
-                    for (int c = 0; c < DCH; ++c) {
-                        const float4 v = *reinterpret_cast<const float4*>(sv + j * P + c * 64 + tx * 4);
-                        acc[i][c][0] = fmaf(p, v.x, acc[i][c][0]); acc[i][c][1] = fmaf(p, v.y, acc[i][c][1]);
-                        acc[i][c][2] = fmaf(p, v.z, acc[i][c][2]); acc[i][c][3] = fmaf(p, v.w, acc[i][c][3]);
+                for (int c = 0; c < DCH; ++c) {
+                    const float4 v = *reinterpret_cast<const float4*>(sv + j * P + c * 64 + tx * 4);
+                    if (in0) {
+                        acc[0][c][0] = fmaf(p0, v.x, acc[0][c][0]); acc[0][c][1] = fmaf(p0, v.y, acc[0][c][1]);
+                        acc[0][c][2] = fmaf(p0, v.z, acc[0][c][2]); acc[0][c][3] = fmaf(p0, v.w, acc[0][c][3]);
+                    }
+                    if (in1) {
+                        acc[1][c][0] = fmaf(p1, v.x, acc[1][c][0]); acc[1][c][1] = fmaf(p1, v.y, acc[1][c][1]);
+                        acc[1][c][2] = fmaf(p1, v.z, acc[1][c][2]); acc[1][c][3] = fmaf(p1, v.w, acc[1][c][3]);
                     }
                 }
+            }
         }
     }
     if (bad) report_paged(a.hdr, 2);

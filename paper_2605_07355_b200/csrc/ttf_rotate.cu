@@ -64,7 +64,8 @@ template <int N> __device__ __forceinline__ float sum_of(const float (&x)[N]) {
     else return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 }
 
-template <typename T, int V, bool APPEND, bool INTER>
+// FULL: the lanes of a head hold exactly its channels
+template <typename T, int V, bool APPEND, bool INTER, bool FULL>
 __global__ void __launch_bounds__(kRotThreads, kRotCtas)
 k_rotate(const __grid_constant__ RotateArgs a, int llanes)
 {
@@ -84,31 +85,14 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
 #pragma unroll
     for (int u = 0; u < NI; ++u) {
         item_at<V>(lane + u * 32, rot, INTER, e[u][0], e[u][1]);
-        in[u][0] = lane + u * 32 < nitems && e[u][0] < D;
-        in[u][1] = lane + u * 32 < nitems && e[u][1] < D;
+        in[u][0] = FULL ? u == 0 : lane + u * 32 < nitems && e[u][0] < D;
+        in[u][1] = FULL ? u == 0 : lane + u * 32 < nitems && e[u][1] < D;
         turned[u] = in[u][0] && e[u][0] < rot;
     }
-    // the coordinates of the pairs ln, ln + 32, ...
-    int axis[kMaxDim / 64];
-    float freq[kMaxDim / 64];
-#pragma unroll
-    for (int i = 0; i < kMaxDim / 64; ++i) {
-        const int j = ln + 32 * i;
-        axis[i] = 0;
-        if (a.axes > 1 && j < pairs) {
-            if (a.cyclic) {
-                const int of = a.axes == 2 ? j >> 1 : j / 3, m = j - of * a.axes;
-                axis[i] = m > 0 && of < (m == 1 ? a.sec1 : a.sec2) ? m : 0;
-            } else axis[i] = j < a.sec0 ? 0 : (j < a.sec0 + a.sec1 ? 1 : 2);
-        }
-    }
-
     pdl_wait();
     int n = a.rows;
     if (APPEND) n = min(n, max(0, __ldcg(a.seq.start + a.seq.seqs)));
     else if (a.count) n = min(n, max(0, __ldcg(a.count)));
-#pragma unroll
-    for (int i = 0; i < kMaxDim / 64; ++i) freq[i] = ln + 32 * i < pairs ? __ldcg(a.freq + ln + 32 * i) : 0.f;
 
     const int warps = gridDim.x * (kRotThreads / 32);
     int parts = 1;                                         // of a row's heads
@@ -118,28 +102,24 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
         const int row = parts > 1 ? unit / parts : unit, part = unit - row * parts;
         const int h0 = parts > 1 ? heads * part / parts : 0, h1 = parts > 1 ? heads * (part + 1) / parts : heads;
 
-        float2 tn[NI][V];                                  // this lane's turns
         bool have = false;
-        auto make_turns = [&]() {
+        auto make_turns = [&]() {                          // cosine and sine of the row's pairs, for all lanes
             __syncwarp();
-#pragma unroll
-            for (int i = 0; i < kMaxDim / 64; ++i) {
-                const int j = ln + 32 * i;
-                if (j < pairs) {
-                    const double w = (double)__ldcg(a.pos + (long long)row * a.axes + axis[i]) * ((double)freq[i] * 0.15915494309189533577);
-                    float c, s;
-                    sincospif((float)(2.0 * (w - rint(w))), &s, &c);
-                    turn[j] = make_float2(c * a.factor, s * a.factor);
+#pragma unroll 1
+            for (int j = ln; j < pairs; j += 32) {
+                int axis = 0;
+                if (a.axes > 1) {
+                    if (a.cyclic) {
+                        const int of = a.axes == 2 ? j >> 1 : j / 3, m = j - of * a.axes;
+                        axis = m > 0 && of < (m == 1 ? a.sec1 : a.sec2) ? m : 0;
+                    } else axis = j < a.sec0 ? 0 : (j < a.sec0 + a.sec1 ? 1 : 2);
                 }
+                const double w = (double)__ldcg(a.pos + (long long)row * a.axes + axis) * ((double)__ldcg(a.freq + j) * 0.15915494309189533577);
+                float c, s;
+                sincospif((float)(2.0 * (w - rint(w))), &s, &c);
+                turn[j] = make_float2(c * a.factor, s * a.factor);
             }
             __syncwarp();
-#pragma unroll
-            for (int u = 0; u < NI; ++u)
-#pragma unroll
-                for (int c = 0; c < V; ++c) {
-                    const int j = (INTER ? e[u][0] >> 1 : e[u][0]) + c;
-                    tn[u][c] = turned[u] && j < pairs ? turn[j] : make_float2(1.f, 0.f);
-                }
         };
 
         // where the row's keys and values go
@@ -169,17 +149,20 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
             constexpr int KIND = decltype(kind_of)::value;
             const int b = max(h0, first), z = min(h1, first + src_of.heads);
             if (b >= z) return;
+            // lane group `sub` takes heads b + sub, b + sub + per_warp, ...; the last job of the warp may be short
+            const int count = z - b, jobs = (count + per_warp - 1) >> (5 - llanes);
+            const bool last_on = sub < count - (jobs - 1) * per_warp;
             const T* src = reinterpret_cast<const T*>(src_of.data) + (long long)row * src_of.row + (long long)(b - first + sub) * src_of.head;
             const long long step = src_of.head << (5 - llanes);
-            int left = z - b - sub;                        // this lane group's heads are there while it is positive
             Raw raw[AHEAD][NI][2];
-            auto fetch = [&](int ahead, Raw (&x)[NI][2]) {
+            auto fetch = [&](int job, Raw (&x)[NI][2]) {
+                const bool on = job + 1 < jobs || (job + 1 == jobs && last_on);
 #pragma unroll
                 for (int u = 0; u < NI; ++u)
 #pragma unroll
                     for (int w = 0; w < 2; ++w) {
                         x[u][w] = Raw{};
-                        if (left > ahead * per_warp && in[u][w]) x[u][w] = load_cg(reinterpret_cast<const Raw*>(src + e[u][w]));
+                        if (on && in[u][w]) x[u][w] = load_cg(reinterpret_cast<const Raw*>(src + e[u][w]));
                     }
                 src += step;
             };
@@ -212,37 +195,44 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
                         // channels of pair c: the vectors' c, or 2c and 2c + 1 of the two vectors in a row
                         const float wu = INTER ? (2 * c < V ? w0[2 * c % V] : w1[2 * c % V]) : w0[c];
                         const float wv = INTER ? (2 * c + 1 < V ? w0[(2 * c + 1) % V] : w1[(2 * c + 1) % V]) : w1[c];
-                        cu[u][c] = wu * tn[u][c].x; su[u][c] = wu * tn[u][c].y;
-                        cv[u][c] = wv * tn[u][c].x; sv[u][c] = -wv * tn[u][c].y;
+                        const int j = (INTER ? e[u][0] >> 1 : e[u][0]) + c;
+                        const float2 t = turned[u] && j < pairs ? turn[j] : make_float2(1.f, 0.f);
+                        cu[u][c] = wu * t.x; su[u][c] = wu * t.y;
+                        cv[u][c] = wv * t.x; sv[u][c] = -wv * t.y;
                     }
                 }
             }
+            store = store && in_bounds(a.hdr, 6, (long long)(row + 1) * heads - 1, (long long)a.rows * heads);
+            T* out[NI][2];
+#pragma unroll
+            for (int u = 0; u < NI; ++u) { out[u][0] = to + e[u][0]; out[u][1] = to + e[u][1]; }
 #pragma unroll 1
-            for (int done = z - b; done > 0; done -= AHEAD * per_warp) {
+            for (int j0 = 0; j0 < jobs; j0 += AHEAD) {
 #pragma unroll
                 for (int y = 0; y < AHEAD; ++y) {
-                    if (done <= y * per_warp) break;       // (the same for the whole warp)
-                    const bool on = left > 0;
-                    Raw now[NI][2];
+                    const int job = j0 + y;
+                    if (job >= jobs) break;                // (the same for the whole warp)
+                    Raw res[NI][2];
+                    if constexpr (KIND == 2) {
 #pragma unroll
-                    for (int u = 0; u < NI; ++u) { now[u][0] = raw[y][u][0]; now[u][1] = raw[y][u][1]; }
-                    fetch(AHEAD, raw[y]);
-                    if constexpr (KIND != 2) {
+                        for (int u = 0; u < NI; ++u) { res[u][0] = raw[y][u][0]; res[u][1] = raw[y][u][1]; }
+                        fetch(job + AHEAD, raw[y]);
+                    } else {
                         float x[NI][2][V];
 #pragma unroll
                         for (int u = 0; u < NI; ++u)
 #pragma unroll
-                            for (int w = 0; w < 2; ++w) unpack<V>(now[u][w], x[u][w], T{});
+                            for (int w = 0; w < 2; ++w) unpack<V>(raw[y][u][w], x[u][w], T{});
+                        fetch(job + AHEAD, raw[y]);
                         float inv[V];
                         inv[0] = 1.f;
                         if (weight) {
                             float part[V];
-#pragma unroll
-                            for (int c = 0; c < V; ++c) part[c] = 0.f;
+                            vmul<V>(part, x[0][0], x[0][0]);
 #pragma unroll
                             for (int u = 0; u < NI; ++u)
 #pragma unroll
-                                for (int w = 0; w < 2; ++w) vfma<V>(part, x[u][w], x[u][w], part);
+                                for (int w = u == 0 ? 1 : 0; w < 2; ++w) vfma<V>(part, x[u][w], x[u][w], part);
                             float ssq = sum_of<V>(part);
                             if (llanes == 3) {             // (heads of 128 channels in bf16)
                                 ssq += __shfl_xor_sync(0xffffffffu, ssq, 4);
@@ -276,24 +266,24 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
                             vmul<V>(t1, qu, su[u]);
                             vfma<V>(t0, pu, cu[u], t0);
                             vfma<V>(t1, pv, cv[u], t1);
+                            float r0[V], r1[V];
 #pragma unroll
                             for (int c = 0; c < V; ++c) {
-                                if (INTER) { x[u][2 * c / V][2 * c % V] = t0[c]; x[u][(2 * c + 1) / V][(2 * c + 1) % V] = t1[c]; }
-                                else { x[u][0][c] = t0[c]; x[u][1][c] = t1[c]; }
+                                if (INTER) { (2 * c < V ? r0 : r1)[2 * c % V] = t0[c]; (2 * c + 1 < V ? r0 : r1)[(2 * c + 1) % V] = t1[c]; }
+                                else { r0[c] = t0[c]; r1[c] = t1[c]; }
                             }
+                            res[u][0] = pack<V>(r0, T{}); res[u][1] = pack<V>(r1, T{});
                         }
-#pragma unroll
-                        for (int u = 0; u < NI; ++u) { now[u][0] = pack<V>(x[u][0], T{}); now[u][1] = pack<V>(x[u][1], T{}); }
                     }
-                    if (on && store && in_bounds(a.hdr, 6, (long long)(row + 1) * heads - 1, (long long)a.rows * heads)) {
+                    if (store && (job + 1 < jobs || last_on)) {
 #pragma unroll
                         for (int u = 0; u < NI; ++u)
 #pragma unroll
                             for (int w = 0; w < 2; ++w)
-                                if (in[u][w]) *reinterpret_cast<Raw*>(to + e[u][w]) = now[u][w];
+                                if (in[u][w]) *reinterpret_cast<Raw*>(out[u][w]) = res[u][w];
                     }
-                    to += to_step;
-                    left -= per_warp;
+#pragma unroll
+                    for (int u = 0; u < NI; ++u) { out[u][0] += to_step; out[u][1] += to_step; }
                 }
             }
         };
@@ -331,8 +321,11 @@ static cudaError_t launch_rotate_v(const RotateArgs& a, cudaStream_t st) {
     const long long most = (long long)a.rows * ((heads + per_warp - 1) / per_warp), warps = kRotThreads / 32;
     long long ctas = (most + warps - 1) / warps;
     if (ctas > sm_count() * kRotCtas) ctas = sm_count() * kRotCtas;
-    return a.interleaved ? launch_pdl(k_rotate<T, V, APPEND, true>, dim3((unsigned)ctas), dim3(kRotThreads), st, a, ll)
-                         : launch_pdl(k_rotate<T, V, APPEND, false>, dim3((unsigned)ctas), dim3(kRotThreads), st, a, ll);
+    const bool full = a.dim == 2 * V << ll;
+    const dim3 grid((unsigned)ctas), block(kRotThreads);
+    if (a.interleaved)
+        return full ? launch_pdl(k_rotate<T, V, APPEND, true, true>, grid, block, st, a, ll) : launch_pdl(k_rotate<T, V, APPEND, true, false>, grid, block, st, a, ll);
+    return full ? launch_pdl(k_rotate<T, V, APPEND, false, true>, grid, block, st, a, ll) : launch_pdl(k_rotate<T, V, APPEND, false, false>, grid, block, st, a, ll);
 }
 cudaError_t launch_rotate(const RotateArgs& a, int dtype, bool append, cudaStream_t st) {
     if (a.rows < 1) return cudaSuccess;
