@@ -15,6 +15,13 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// 16 bytes into shared memory, zeros where `bytes` is 0 (the address is inside the cache all the same)
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 template <int D> struct JoinSpace {
     static constexpr int OP = D + 4;                       // floats of a row
     float m[kMmaWarps][kMmaRows], l[kMmaWarps][kMmaRows];  // every warp's maxima and sums
@@ -26,7 +33,7 @@ template <int D> struct JoinSpace {
 
 // Adds up the warps' sums of the tile's `nrow` rows, then those of the ranks, and writes the rows.  Every thread of the CTA;
 // jn.m, jn.l and jn.o are visible to all, and with a cluster every thread has arrived at its barrier once before.
-template <int D>
+template <int D, typename T = bf16_t>
 __device__ __forceinline__ void join_rows(const AttendArgs& a, JoinSpace<D>& jn, const SeqRange& r, int row0, int nrow, int hk,
                                           int lsplit, int rank) {
     constexpr int OP = JoinSpace<D>::OP, Q4 = D / 4;
@@ -35,9 +42,9 @@ __device__ __forceinline__ void join_rows(const AttendArgs& a, JoinSpace<D>& jn,
         const int token = (row0 + row) / a.group, head = hk * a.group + (row0 + row) - token * a.group;
         if (d >= dim || !in_bounds(a.hdr, 8, (long long)r.first + token, a.seq.rows)) return;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        uint2 w = make_uint2(0, 0);
-        if (sum != 0.f) w = make_uint2(bf16_pair(v.x * inv, v.y * inv), bf16_pair(v.z * inv, v.w * inv));
-        *reinterpret_cast<uint2*>(reinterpret_cast<bf16_t*>(a.out.data) + (long long)(r.first + token) * a.out.row + (long long)head * a.out.head + d) = w;
+        float x[4] = {0.f, 0.f, 0.f, 0.f};                 // (no slot seen: zero)
+        if (sum != 0.f) { x[0] = v.x * inv; x[1] = v.y * inv; x[2] = v.z * inv; x[3] = v.w * inv; }
+        *reinterpret_cast<typename VecIO<T, 4>::Raw*>(reinterpret_cast<T*>(a.out.data) + (long long)(r.first + token) * a.out.row + (long long)head * a.out.head + d) = pack<4>(x, T{});
     };
     if (lsplit) { __syncwarp(); cluster_wait(); }          // every rank is running
     for (int e = tid; e < nrow * Q4; e += kMmaThreads) {

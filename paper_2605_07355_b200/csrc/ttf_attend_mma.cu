@@ -24,7 +24,6 @@
 
 namespace ttf {
 
-
 template <int DC> struct MmaShape {                        // DC: 32-channel pieces of a head (even)
     static constexpr int D = DC * 32;
     static constexpr int PIECES = 4 * DC;                  // 16-byte pieces of a lane in a stage: 2 slots x DC of K, 4 x DC / 2 of V
@@ -34,12 +33,6 @@ template <int DC> struct MmaShape {                        // DC: 32-channel pie
     static constexpr int OP = D + 4;                       // floats of a row that warps exchange
 };
 
-// 16 bytes into shared memory, zeros where `bytes` is 0 (the address is inside the cache all the same)
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
-    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ uint4 lds128(uint32_t addr) {
     uint4 v;
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");

@@ -1,13 +1,13 @@
-// Attention of new rows over a paged cache in fp32 arithmetic: fp32 caches, and bf16 heads that the matrix instructions
-// cannot take (channels not a multiple of 8, unaligned strides).
+// Attention of new rows over a paged cache in fp32 arithmetic, for heads that fit no 16-byte pieces: bf16 heads that the matrix
+// instructions cannot take (channels not a multiple of 8, unaligned strides), fp32 heads in the same way.
 //
 //   o = sum_s exp2(t_s - m) v_s / sum_s exp2(t_s - m),   t_s = scale log2(e) <q, k_s>,   m the running maximum
 //
 // One CTA takes 32 packed rows (tokens x query heads of a group, so that a group reads its keys and values once) of one
 // sequence and key head, and walks the visible slots 32 at a time: scores as 2 x 2 dot products per thread from shared
 // memory, one softmax step with eight threads per row, then 2 rows x D / 16 channels of the sum per thread.  The next
-// block is loaded into registers meanwhile, its pages are looked up one block earlier.  Bound by the fp32 pipes (four
-// shared-memory loads feed sixteen FMAs) and, with few rows, by latency: the CTAs of a cluster then share the slots and
+// block is loaded into registers meanwhile, its pages are looked up one block earlier.  Bound by shared memory (four
+// loads of 16 bytes feed sixteen FMAs) and, with few rows, by latency: the CTAs of a cluster then share the slots and
 // join their sums through distributed shared memory.
 //
 // A slot that a row does not see takes no part in that row's sum, whatever it holds.
@@ -23,12 +23,6 @@ template <int DCH> struct SimpleShape {
     static constexpr int P = DCH * 64 + 4;                 // floats of a shared row (the pad spreads rows over the banks)
     static constexpr int FLOATS = 3 * 32 * P + 32 * 33 + 4 * 32;
 };
-
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-}
 
 template <typename T, int V, int DCH>
 __global__ void __launch_bounds__(kSimpleThreads)
@@ -152,7 +146,11 @@ k_attend_simple(const __grid_constant__ AttendArgs a, int lsplit)
         __syncthreads();
         if (blk + 1 < my_z) load();
         look_up(blk + 2);
-        float dot[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
+        float4 sums[2][2];                                 // (four chains per dot product)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) sums[i][j] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
         for (int d = 0; d < D; d += 4) {                   // (channels from D to the next multiple of 4 are zeros in both)
             float4 q4[2], k4[2];
@@ -165,8 +163,8 @@ k_attend_simple(const __grid_constant__ AttendArgs a, int lsplit)
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    dot[i][j] = fmaf(q4[i].x, k4[j].x, dot[i][j]); dot[i][j] = fmaf(q4[i].y, k4[j].y, dot[i][j]);
-                    dot[i][j] = fmaf(q4[i].z, k4[j].z, dot[i][j]); dot[i][j] = fmaf(q4[i].w, k4[j].w, dot[i][j]);
+                    sums[i][j].x = fmaf(q4[i].x, k4[j].x, sums[i][j].x); sums[i][j].y = fmaf(q4[i].y, k4[j].y, sums[i][j].y);
+                    sums[i][j].z = fmaf(q4[i].z, k4[j].z, sums[i][j].z); sums[i][j].w = fmaf(q4[i].w, k4[j].w, sums[i][j].w);
                 }
         }
 #pragma unroll
@@ -174,7 +172,8 @@ k_attend_simple(const __grid_constant__ AttendArgs a, int lsplit)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int s = base + tx + 16 * j;
-                ss[(ty + 16 * i) * 33 + tx + 16 * j] = s >= mine[i].lo && s < mine[i].hi ? dot[i][j] : -INFINITY;
+                const float dot = (sums[i][j].x + sums[i][j].y) + (sums[i][j].z + sums[i][j].w);
+                ss[(ty + 16 * i) * 33 + tx + 16 * j] = s >= mine[i].lo && s < mine[i].hi ? dot : -INFINITY;
             }
         __syncthreads();
         {                                                  // softmax step: row lr, slots lc, lc + 8, ...
@@ -202,11 +201,14 @@ k_attend_simple(const __grid_constant__ AttendArgs a, int lsplit)
             }
         }
         __syncthreads();
-        const float f0 = s_f[ty], f1 = s_f[ty + 16];
+        // the block's products are summed apart and then added: over thousands of slots one chain would lose digits
+        float part[2][DCH][4];
 #pragma unroll
-        for (int c = 0; c < DCH; ++c)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { acc[0][c][e] *= f0; acc[1][c][e] *= f1; }
+            for (int c = 0; c < DCH; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) part[i][c][e] = 0.f;
         const int a0 = max(mine[0].lo - base, 0), z0 = min(mine[0].hi - base, kSimpleKeys);
         const int a1 = max(mine[1].lo - base, 0), z1 = min(mine[1].hi - base, kSimpleKeys);
         if (a0 == 0 && a1 == 0 && z0 == kSimpleKeys && z1 == kSimpleKeys) {
@@ -216,10 +218,10 @@ k_attend_simple(const __grid_constant__ AttendArgs a, int lsplit)
 #pragma unroll
                 for (int c = 0; c < DCH; ++c) {
                     const float4 v = *reinterpret_cast<const float4*>(sv + j * P + c * 64 + tx * 4);
-                    acc[0][c][0] = fmaf(p0, v.x, acc[0][c][0]); acc[0][c][1] = fmaf(p0, v.y, acc[0][c][1]);
-                    acc[0][c][2] = fmaf(p0, v.z, acc[0][c][2]); acc[0][c][3] = fmaf(p0, v.w, acc[0][c][3]);
-                    acc[1][c][0] = fmaf(p1, v.x, acc[1][c][0]); acc[1][c][1] = fmaf(p1, v.y, acc[1][c][1]);
-                    acc[1][c][2] = fmaf(p1, v.z, acc[1][c][2]); acc[1][c][3] = fmaf(p1, v.w, acc[1][c][3]);
+                    part[0][c][0] = fmaf(p0, v.x, part[0][c][0]); part[0][c][1] = fmaf(p0, v.y, part[0][c][1]);
+                    part[0][c][2] = fmaf(p0, v.z, part[0][c][2]); part[0][c][3] = fmaf(p0, v.w, part[0][c][3]);
+                    part[1][c][0] = fmaf(p1, v.x, part[1][c][0]); part[1][c][1] = fmaf(p1, v.y, part[1][c][1]);
+                    part[1][c][2] = fmaf(p1, v.z, part[1][c][2]); part[1][c][3] = fmaf(p1, v.w, part[1][c][3]);
                 }
             }
         } else {
@@ -233,16 +235,23 @@ k_attend_simple(const __grid_constant__ AttendArgs a, int lsplit)
                 for (int c = 0; c < DCH; ++c) {
                     const float4 v = *reinterpret_cast<const float4*>(sv + j * P + c * 64 + tx * 4);
                     if (in0) {
-                        acc[0][c][0] = fmaf(p0, v.x, acc[0][c][0]); acc[0][c][1] = fmaf(p0, v.y, acc[0][c][1]);
-                        acc[0][c][2] = fmaf(p0, v.z, acc[0][c][2]); acc[0][c][3] = fmaf(p0, v.w, acc[0][c][3]);
+                        part[0][c][0] = fmaf(p0, v.x, part[0][c][0]); part[0][c][1] = fmaf(p0, v.y, part[0][c][1]);
+                        part[0][c][2] = fmaf(p0, v.z, part[0][c][2]); part[0][c][3] = fmaf(p0, v.w, part[0][c][3]);
                     }
                     if (in1) {
-                        acc[1][c][0] = fmaf(p1, v.x, acc[1][c][0]); acc[1][c][1] = fmaf(p1, v.y, acc[1][c][1]);
-                        acc[1][c][2] = fmaf(p1, v.z, acc[1][c][2]); acc[1][c][3] = fmaf(p1, v.w, acc[1][c][3]);
+                        part[1][c][0] = fmaf(p1, v.x, part[1][c][0]); part[1][c][1] = fmaf(p1, v.y, part[1][c][1]);
+                        part[1][c][2] = fmaf(p1, v.z, part[1][c][2]); part[1][c][3] = fmaf(p1, v.w, part[1][c][3]);
                     }
                 }
             }
         }
+        const float f[2] = {s_f[ty], s_f[ty + 16]};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int c = 0; c < DCH; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][c][e] = fmaf(acc[i][c][e], f[i], part[i][c][e]);
     }
     if (bad) report_paged(a.hdr, 2);
     __syncthreads();
@@ -351,7 +360,7 @@ cudaError_t launch_attend_simple(const AttendArgs& a, int dtype, cudaStream_t st
                       aligned_to(a.out.data, a.out.row, a.out.head, 0, 4, item) &&
                       aligned_to(a.cache.k, a.cache.k_page, a.cache.k_row, a.cache.k_head, 4, item) &&
                       aligned_to(a.cache.v, a.cache.v_page, a.cache.v_row, a.cache.v_head, 4, item);
-    if (dtype == TTF_DTYPE_F32) return four ? launch_simple_v<float, 4>(a, st) : launch_simple_v<float, 1>(a, st);
+    if (dtype == TTF_DTYPE_F32) return launch_simple_v<float, 1>(a, st);
     return four ? launch_simple_v<bf16_t, 4>(a, st) : launch_simple_v<bf16_t, 1>(a, st);
 }
 

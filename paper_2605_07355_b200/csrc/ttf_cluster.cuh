@@ -1,4 +1,4 @@
-// Thread-block clusters: rank, barrier and writes into another CTA's shared memory, as inline PTX.
+// Thread-block clusters: rank, barrier, writes into and reads from another CTA's shared memory, as inline PTX.
 #pragma once
 
 #include <stdint.h>
@@ -24,6 +24,11 @@ __device__ __forceinline__ void st_cluster_f32(uint32_t remote, float v) {
 }
 __device__ __forceinline__ void st_cluster_u32(uint32_t remote, uint32_t v) {
     asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(remote), "r"(v) : "memory");
+}
+__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
 }
 
 }  // namespace ttf

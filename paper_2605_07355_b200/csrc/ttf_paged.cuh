@@ -74,6 +74,9 @@ struct AttendArgs {
 cudaError_t launch_attend(const AttendArgs& a, int dtype, cudaStream_t st);
 bool attend_tc_takes(const AttendArgs& a, int dtype);
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t st);
+bool attend_f32_takes(const AttendArgs& a, int dtype);
+cudaError_t launch_attend_f32(const AttendArgs& a, cudaStream_t st);
+cudaError_t launch_attend_few32(const AttendArgs& a, cudaStream_t st);
 bool attend_few_takes(const AttendArgs& a, int dtype);
 cudaError_t launch_attend_few(const AttendArgs& a, cudaStream_t st);
 // TMA tiles of the cache: 64 channels x `rows` slots of one head and page, 128-byte swizzle, zeros beyond the head
