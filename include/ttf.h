@@ -398,8 +398,11 @@ int ttf_cache_append(const ttf_heads* k, const ttf_heads* v, const ttf_heads* q,
  *   out[i, h] = sum over the visible slots s of softmax_s(scale * <q[i, h], k[s, h / group]>) v[s, h / group]
  * with group = q->heads / cache->heads (a whole number).  Row i at slot c sees every slot of its sequence with causal = 0,
  * the slots up to c with causal = 1, of these only those above c - window where window > 0.  A row that sees nothing is
- * zero.  Slots that no row of the sequence sees may hold anything, NaN included.  One row per sequence (decoding) to
- * thousands (prefill, segments) in any mixture; the kernel is chosen by the sizes that the host knows.  head_dim 1 to 256.
+ * zero.  Slots that no row of the sequence sees may hold anything, NaN included.  A value that is infinite or NaN in a slot
+ * that some row sees always reaches those rows; in bf16 it may make rows of the same sequence NaN that do not see the slot
+ * (a block of rows is multiplied at once, their weight of zero with it), in fp32 it does not.  One row per sequence
+ * (decoding) to thousands (prefill, segments) in any mixture; the kernel is chosen by the sizes that the host knows, so that
+ * `rows` far above the rows that are there costs speed where every sequence has a few.  head_dim 1 to 256.
  */
 int ttf_attend(const ttf_heads* q, const ttf_sequences* sequences, const ttf_cache* cache, float scale, int causal,
                int window, const ttf_heads* out, ttf_stream_t stream);

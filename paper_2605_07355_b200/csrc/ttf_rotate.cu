@@ -10,7 +10,7 @@
 // channels, multiplied with the norm's weight, in registers for all heads:
 //   u' = inv (x_u (w_u c) - x_v (w_v s)),   v' = inv (x_v (w_v c) + x_u (w_u s)).
 // (Turns and weights re-read from shared memory for every head cost as much as the rest: with CTAs that share rows the
-// clip of 2703 rows, 32 + 8 heads of 128 took 21.7 us, 12.0 without norm and rotation; this form AAA.)  A head is an item of
+// clip of 2703 rows, 32 + 8 heads of 128 took 21.7 us, 12.0 without norm and rotation; this form 14.6.)  A head is an item of
 // two V-channel vectors per lane (for the half layout the two halves of V pairs), the lanes of a head are the power of two
 // that covers it, and a warp holds 32 / lanes heads; the next heads are on their way while the present ones are worked on.
 // Rows are dealt out to the warps by the number that only the device knows, so worst-case buffers cost nothing.
