@@ -308,7 +308,8 @@ static inline double ttf_reduction_ratio(long long P, int F, int N) {
  *
  * Like the rest of the library they only enqueue work and are deterministic; they use no scratch at all, so that calls on
  * different streams and captured graphs share nothing.  Sums, softmax statistics and accumulators are fp32, results are
- * rounded once.  Inputs may not overlap outputs except where stated.
+ * rounded once.  Inputs may not overlap outputs except where stated.  An input's strides may be zero (a broadcast axis), those of an
+ * output's axes of more than one element may not.
  */
 
 /* The heads of a sequence of rows: element d of head h of row i is data[i * row_stride + h * head_stride + d] (strides in

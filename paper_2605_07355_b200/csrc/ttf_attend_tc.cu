@@ -529,20 +529,24 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------
-static bool tma_ok(const void* p, long long s0, long long s1, long long s2) {
-    auto fine = [](long long s) { return s >= 0 && s % 8 == 0 && s < (1LL << 38); };
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && fine(s0) && fine(s1) && fine(s2);
+// an axis of `n` elements, `s` elements apart, that a map can have: a broadcast axis (no step between its elements) it cannot
+static bool axis_ok(long long n, long long s) { return (n == 1 || s > 0) && s >= 0 && s % 8 == 0 && s < (1LL << 38); }
+static bool rows_fit(const HeadsView& h, int rows) {
+    return reinterpret_cast<uintptr_t>(h.data) % 16 == 0 && axis_ok(rows, h.row) && axis_ok(h.heads, h.head);
 }
 bool cache_maps_fit(const AttendArgs& a) {
-    return tma_ok(a.cache.k, a.cache.k_page, a.cache.k_row, a.cache.k_head) &&
-           tma_ok(a.cache.v, a.cache.v_page, a.cache.v_row, a.cache.v_head) && encode_fn() != nullptr;
+    const CacheView& c = a.cache;
+    auto fit = [&](const void* p, long long page, long long row, long long head) {
+        return reinterpret_cast<uintptr_t>(p) % 16 == 0 && axis_ok(c.pages, page) && axis_ok(c.page.d, row) && axis_ok(c.heads, head);
+    };
+    return fit(c.k, c.k_page, c.k_row, c.k_head) && fit(c.v, c.v_page, c.v_row, c.v_head) && encode_fn() != nullptr;
 }
 
 bool attend_tc_takes(const AttendArgs& a, int dtype) {
     const int page = (int)a.cache.page.d;
     return dtype == TTF_DTYPE_BF16 && a.cache.dim % 8 == 0 && a.cache.dim <= 128 && a.group <= kAtRows && a.scale > 0.f &&
            page % 8 == 0 && (page <= kAtSlots || page % kAtSlots == 0) &&
-           tma_ok(a.q.data, a.q.row, a.q.head, 0) && tma_ok(a.out.data, a.out.row, a.out.head, 0) && cache_maps_fit(a);
+           rows_fit(a.q, a.seq.rows) && rows_fit(a.out, a.seq.rows) && cache_maps_fit(a);
 }
 
 // a map over axes of `n` elements with strides of `s` elements (0: an axis of one element, whose stride does not matter)

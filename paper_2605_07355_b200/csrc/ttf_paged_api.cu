@@ -56,6 +56,11 @@ static int check_heads(const ttf_heads* h, int rows) {
     if (h->heads > 65535 || (long long)rows * h->heads >= (1LL << 31)) return TTF_ERR_UNSUPPORTED;
     return reachable(rows, h->row_stride, h->heads, h->head_stride, 0, 0) ? TTF_OK : TTF_ERR_UNSUPPORTED;
 }
+// no two elements of an output in one place
+static bool apart(long long n0, long long s0, long long n1, long long s1, long long n2, long long s2) {
+    return (n0 == 1 || s0) && (n1 == 1 || s1) && (n2 == 1 || s2);
+}
+static bool apart(const ttf_heads* h, int rows) { return !h || apart(rows, h->row_stride, h->heads, h->head_stride, 1, 0); }
 static bool known_dtype(int dtype) { return dtype == TTF_DTYPE_F32 || dtype == TTF_DTYPE_BF16; }
 
 static int check_rotation(const ttf_rotation* r, int head_dim, const int* positions) {
@@ -127,6 +132,7 @@ int ttf_rotate(const ttf_heads* q, const ttf_heads* k, int head_dim, int dtype, 
     for (const ttf_heads* h : {q, k, out_q, out_k})
         if (h) TTF_CHECK(check_heads(h, rows));
     if ((q && q->heads != out_q->heads) || (k && k->heads != out_k->heads)) return TTF_ERR_INVALID_ARG;
+    if (!apart(out_q, rows) || !apart(out_k, rows)) return TTF_ERR_INVALID_ARG;
     RotateArgs a = {};
     TTF_CHECK(paged_words(&a.hdr));
     a.q = ttf::view(q, rows); a.k = ttf::view(k, rows); a.out_q = ttf::view(out_q, rows); a.out_k = ttf::view(out_k, rows);
@@ -149,6 +155,8 @@ int ttf_cache_append(const ttf_heads* k, const ttf_heads* v, const ttf_heads* q,
     for (const ttf_heads* h : {k, v, q, out_q})
         if (h) TTF_CHECK(check_heads(h, sequences->rows));
     if (k->heads != cache->heads || v->heads != cache->heads || (q && q->heads != out_q->heads)) return TTF_ERR_INVALID_ARG;
+    if (!apart(out_q, sequences->rows) || !apart(cache->pages, cache->k_page, cache->page_size, cache->k_row, cache->heads, cache->k_head) ||
+        !apart(cache->pages, cache->v_page, cache->page_size, cache->v_row, cache->heads, cache->v_head)) return TTF_ERR_INVALID_ARG;
     RotateArgs a = {};
     TTF_CHECK(paged_words(&a.hdr));
     const int rows = sequences->rows;
@@ -168,7 +176,7 @@ int ttf_attend(const ttf_heads* q, const ttf_sequences* sequences, const ttf_cac
     TTF_CHECK(check_cache(cache));
     TTF_CHECK(check_sequences(sequences));
     for (const ttf_heads* h : {q, out}) TTF_CHECK(check_heads(h, sequences->rows));
-    if (q->heads != out->heads || q->heads % cache->heads) return TTF_ERR_INVALID_ARG;
+    if (q->heads != out->heads || q->heads % cache->heads || !apart(out, sequences->rows)) return TTF_ERR_INVALID_ARG;
     AttendArgs a = {};
     TTF_CHECK(paged_words(&a.hdr));
     a.q = ttf::view(q, sequences->rows); a.out = ttf::view(out, sequences->rows); a.seq = ttf::view(sequences); a.cache = ttf::view(cache);
