@@ -248,6 +248,8 @@ __device__ __forceinline__ bool find_tile(const AttendArgs& a, const Cut& cut, i
             const int src = __ffs(m) - 1;
             t.seq = s0 + src;
             t.tile = want - __shfl_sync(0xffffffffu, upto - c, src);
+            // (overlapping sequences, which are reported, may add up to more than 31 bits)
+            if ((unsigned)t.tile >= (unsigned)__shfl_sync(0xffffffffu, c, src)) return false;
             t.r.first = __shfl_sync(0xffffffffu, r.first, src);
             t.r.n = __shfl_sync(0xffffffffu, r.n, src);
             t.r.length = __shfl_sync(0xffffffffu, r.length, src);
