@@ -272,3 +272,31 @@ def test_checked_build():
     env = dict(os.environ, TTF_B200_LIB=build.build(checked=True))
     out = subprocess.run([sys.executable, "-c", CHECKED], env=env, cwd=root, capture_output=True, text=True, timeout=900)
     assert out.returncode == 0 and "checked build ok" in out.stdout, out.stdout[-2000:] + out.stderr[-4000:]
+
+
+FIRST = """
+import torch
+import paper_2605_07355_b200 as P
+from tests.test_gpu_attend import Batch
+b = Batch({new}, [40, 300], 16, 8, 2, 128, "{dtype}")
+q, k, v, st, ln, tb = b.on_device()
+out, turned = torch.zeros_like(q), torch.zeros_like(q)
+pos, freq = torch.arange(q.shape[0], device="cuda", dtype=torch.int32), torch.rand(64, device="cuda")
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    P.ttf_rotate(q, None, pos, freq, out_q=turned)
+    P.ttf_attend(q, k, v, st, ln, tb, b.scale, out=out)
+g.replay()
+assert P.ttf_paged_status() == 0
+m = b.start[-1]
+assert torch.equal(P.ttf_attend(q, k, v, st, ln, tb, b.scale)[:m], out[:m])
+assert torch.equal(P.ttf_rotate(q, None, pos, freq)[0], turned)
+"""
+
+
+@pytest.mark.parametrize("new,dtype", [([1, 1], "bf16"), ([3, 200], "bf16"), ([1, 1], "f32"), ([3, 200], "f32")])
+def test_a_process_may_begin_with_a_capture(new, dtype):
+    r = subprocess.run([sys.executable, "-c", FIRST.format(new=new, dtype=dtype)], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
+                       capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
