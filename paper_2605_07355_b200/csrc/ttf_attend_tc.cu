@@ -16,10 +16,13 @@
 // only where a maximum has grown by more than 8 (in powers of two: weights stay below 2^8, l and O carry the same factor, and
 // nothing is lost, since bf16 and fp32 keep their relative precision), which after the first blocks is rare.
 //
-// Bound by the chain of a tile: a block of 128 slots takes 1.9 to 2.2 us with both tiles, 1.5 at the rate of a library product
-// (scores come 64 slots at a time, which reads Q once more, so that the softmax of one half runs under the products of the
-// other), and a CTA 6 us more before its first scores and after its last.  4096 new rows over 16384 slots, 32 heads of 128: 889 us,
-// 1.08 PFLOP/s, about 1010 under the power cap (1196 with scores handed over whole; with one warp for both tiles' products 1330).
+// Bound by the tensor pipe's operands and the chain of a tile together: half a block takes some 2090 cycles, of which a tile's
+// softmax waits 600 for its scores and spends 40 on loading them, 290 on the maximum, 1000 on exponentials, sums and conversion;
+// the thread that issues is held 1390 of them by its twelve products (those of the scores are 64 slots wide and so read Q from
+// shared memory twice a block, 1.5 times what they multiply).  A CTA adds 6 us before its first scores and after its last.
+// 4096 new rows over 16384 slots, 32 heads of 128: 890 us, 1.08 PFLOP/s, about 1010 under the power cap.  Slower were: scores
+// handed over whole 1205, two threads a row 1022, one warp for both tiles' products 1330, an eighth of the exponentials on the
+// fp32 pipe 917; scores and sums issued by two threads a tile made no difference.
 //
 // Few tiles over many slots: the CTAs of a cluster share the blocks, and each finishes a part of the rows from what all of them
 // send into its shared memory.
