@@ -400,14 +400,14 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
                 }
             }
             const float ref = m == -INFINITY ? 0.f : m;
-            const float2 c2 = make_float2(c, c), ref2 = make_float2(-ref, -ref);
-            float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            const Pair c2 = pair_of(c, c), ref2 = pair_of(-ref, -ref);
+            Pair sum[2] = {0, 0};
             uint32_t p[32];
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
-                const float2 t = fma2(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), c2, ref2);
+                const float2 t = both_of(fma2(pair_of(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), c2, ref2));
                 const float2 w = make_float2(exp2_approx(t.x), exp2_approx(t.y));
-                sum[e & 1] = add2(sum[e & 1], w);
+                sum[e & 1] = add2(sum[e & 1], pair_of(w.x, w.y));
                 p[e] = bf16_pair(w.x, w.y);
             }
             tmem_st32(sb, p);
@@ -415,7 +415,7 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&bar_p[x][b]);
-            const float2 both = add2(sum[0], sum[1]);
+            const float2 both = both_of(add2(sum[0], sum[1]));
             l += both.x + both.y;
         }
         if (n > 0 && ok) wait(&bar_o[x], 0);               // O is complete

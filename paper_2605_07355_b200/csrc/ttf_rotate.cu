@@ -10,7 +10,7 @@
 // channels, multiplied with the norm's weight, in registers for all heads:
 //   u' = inv (x_u (w_u c) - x_v (w_v s)),   v' = inv (x_v (w_v c) + x_u (w_u s)).
 // (Turns and weights re-read from shared memory for every head cost as much as the rest: with CTAs that share rows the
-// clip of 2703 rows, 32 + 8 heads of 128 took 21.7 us, 12.0 without norm and rotation; this form 14.6.)  A head is an item of
+// clip of 2703 rows, 32 + 8 heads of 128 took 21.7 us, 12.0 without norm and rotation; this form 14.5.)  A head is an item of
 // two V-channel vectors per lane (for the half layout the two halves of V pairs), the lanes of a head are the power of two
 // that covers it, and a warp holds 32 / lanes heads; the next heads are on their way while the present ones are worked on.
 // Rows are dealt out to the warps by the number that only the device knows, so worst-case buffers cost nothing.
@@ -36,32 +36,15 @@ template <int V> __device__ __forceinline__ void item_at(int it, int rot, int in
     e1 = halves ? rot / 2 + it * V : e0 + V;
 }
 
-// y[] = x[] * b[] (+ c[]) over N channels
-template <int N> __device__ __forceinline__ void vmul(float (&y)[N], const float (&x)[N], const float (&b)[N]) {
-    if constexpr (N == 1) y[0] = x[0] * b[0];
-    else {
-#pragma unroll
-        for (int i = 0; i < N; i += 2) {
-            const float2 d = mul2(make_float2(x[i], x[i + 1]), make_float2(b[i], b[i + 1]));
-            y[i] = d.x; y[i + 1] = d.y;
-        }
-    }
-}
-template <int N> __device__ __forceinline__ void vfma(float (&y)[N], const float (&x)[N], const float (&b)[N], const float (&c)[N]) {
-    if constexpr (N == 1) y[0] = fmaf(x[0], b[0], c[0]);
-    else {
-#pragma unroll
-        for (int i = 0; i < N; i += 2) {
-            const float2 d = fma2(make_float2(x[i], x[i + 1]), make_float2(b[i], b[i + 1]), make_float2(c[i], c[i + 1]));
-            y[i] = d.x; y[i + 1] = d.y;
-        }
-    }
-}
-template <int N> __device__ __forceinline__ float sum_of(const float (&x)[N]) {
-    if constexpr (N == 1) return x[0];
-    else if constexpr (N == 2) return x[0] + x[1];
-    else if constexpr (N == 4) return (x[0] + x[1]) + (x[2] + x[3]);
-    else return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+// the sum over the lanes of a head
+__device__ __forceinline__ float head_sum(float x, int lanes, int llanes) {
+    if (llanes == 3) {                                     // (heads of 128 channels in bf16)
+        x += __shfl_xor_sync(0xffffffffu, x, 4);
+        x += __shfl_xor_sync(0xffffffffu, x, 2);
+        x += __shfl_xor_sync(0xffffffffu, x, 1);
+    } else
+        for (int o = lanes >> 1; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
 }
 
 // FULL: the lanes of a head hold exactly its channels
@@ -202,6 +185,22 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
                     }
                 }
             }
+            // as pairs: of neighbours in the half layout, else of (u, v)
+            constexpr int NP = V == 1 ? 1 : (INTER ? V : V / 2);
+            [[maybe_unused]] Pair cu2[NI][NP], sv2[NI][NP], cv2[NI][NP], su2[NI][NP];
+            if constexpr (V > 1 && KIND != 2) {
+#pragma unroll
+                for (int u = 0; u < NI; ++u)
+#pragma unroll
+                    for (int c = 0; c < NP; ++c) {
+                        cu2[u][c] = INTER ? pair_of(cu[u][c], cv[u][c]) : pair_of(cu[u][2 * c], cu[u][2 * c + 1]);
+                        sv2[u][c] = INTER ? pair_of(sv[u][c], su[u][c]) : pair_of(sv[u][2 * c], sv[u][2 * c + 1]);
+                        if constexpr (!INTER) {
+                            cv2[u][c] = pair_of(cv[u][2 * c], cv[u][2 * c + 1]);
+                            su2[u][c] = pair_of(su[u][2 * c], su[u][2 * c + 1]);
+                        }
+                    }
+            }
             store = store && in_bounds(a.hdr, 6, (long long)(row + 1) * heads - 1, (long long)a.rows * heads);
             T* out[NI][2];
 #pragma unroll
@@ -217,62 +216,80 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
 #pragma unroll
                         for (int u = 0; u < NI; ++u) { res[u][0] = raw[y][u][0]; res[u][1] = raw[y][u][1]; }
                         fetch(job + AHEAD, raw[y]);
-                    } else {
-                        float x[NI][2][V];
+                    } else if constexpr (V > 1) {
+                        Pair x[NI][2][V / 2];
 #pragma unroll
                         for (int u = 0; u < NI; ++u)
 #pragma unroll
-                            for (int w = 0; w < 2; ++w) unpack<V>(raw[y][u][w], x[u][w], T{});
+                            for (int w = 0; w < 2; ++w) unpack_pairs<V>(raw[y][u][w], x[u][w], T{});
                         fetch(job + AHEAD, raw[y]);
-                        float inv[V];
-                        inv[0] = 1.f;
+                        Pair inv = 0;
                         if (weight) {
-                            float part[V];
-                            vmul<V>(part, x[0][0], x[0][0]);
+                            Pair part[V / 2];
 #pragma unroll
-                            for (int u = 0; u < NI; ++u)
+                            for (int c = 0; c < V / 2; ++c) {
+                                part[c] = mul2(x[0][0][c], x[0][0][c]);
 #pragma unroll
-                                for (int w = u == 0 ? 1 : 0; w < 2; ++w) vfma<V>(part, x[u][w], x[u][w], part);
-                            float ssq = sum_of<V>(part);
-                            if (llanes == 3) {             // (heads of 128 channels in bf16)
-                                ssq += __shfl_xor_sync(0xffffffffu, ssq, 4);
-                                ssq += __shfl_xor_sync(0xffffffffu, ssq, 2);
-                                ssq += __shfl_xor_sync(0xffffffffu, ssq, 1);
-                            } else
-                                for (int o = lanes >> 1; o > 0; o >>= 1) ssq += __shfl_xor_sync(0xffffffffu, ssq, o);
-                            inv[0] = rsqrtf(fmaf(ssq, a.inv_dim, a.eps));
+                                for (int u = 0; u < NI; ++u)
+#pragma unroll
+                                    for (int w = u == 0 ? 1 : 0; w < 2; ++w) part[c] = fma2(x[u][w][c], x[u][w][c], part[c]);
+                            }
+#pragma unroll
+                            for (int c = V / 4; c > 0; c >>= 1)
+#pragma unroll
+                                for (int d = 0; d < c; ++d) part[d] = add2(part[d], part[d + c]);
+                            const float2 two = both_of(part[0]);
+                            const float root = rsqrtf(fmaf(head_sum(two.x + two.y, lanes, llanes), a.inv_dim, a.eps));
+                            inv = pair_of(root, root);
                         }
 #pragma unroll
-                        for (int c = 1; c < V; ++c) inv[c] = inv[0];
+                        for (int u = 0; u < NI; ++u) {
+#pragma unroll
+                            for (int c = 0; c < (INTER ? V : V / 2); ++c) {
+                                // half layout: pairs of u and pairs of v; else (u, v) and (v, u)
+                                Pair pu = INTER ? x[u][2 * c / V][c % (V / 2)] : x[u][0][c], pv = INTER ? 0 : x[u][1][c];
+                                if (weight) { pu = mul2(pu, inv); if (!INTER) pv = mul2(pv, inv); }
+                                Pair qu = pu, qv = pv;
+                                if (INTER) { const float2 t = both_of(pu); qv = pair_of(t.y, t.x); }
+                                // (channels that do not turn: their neighbour, whatever it holds, plays no part)
+                                if (rot < D) {
+                                    const bool t = turned[u] && (!INTER || (e[u][0] >> 1) + c < pairs);
+                                    qu = t ? qu : 0; qv = t ? qv : 0;
+                                }
+                                const float2 y0 = both_of(fma2(pu, cu2[u][c], mul2(qv, sv2[u][c])));
+                                const float2 y1 = INTER ? y0 : both_of(fma2(pv, cv2[u][c], mul2(qu, su2[u][c])));
+                                auto put = [&](Raw& r, int i, float2 y) {
+                                    uint32_t* const to = reinterpret_cast<uint32_t*>(&r);
+                                    if constexpr (sizeof(T) == 2) to[i] = bf16_pair(y.x, y.y);
+                                    else { to[2 * i] = __float_as_uint(y.x); to[2 * i + 1] = __float_as_uint(y.y); }
+                                };
+                                if (INTER) put(res[u][2 * c / V], c % (V / 2), y0);
+                                else { put(res[u][0], c, y0); put(res[u][1], c, y1); }
+                            }
+                        }
+                    } else {                               // single channels
+                        float x[NI][2];
+#pragma unroll
+                        for (int u = 0; u < NI; ++u)
+#pragma unroll
+                            for (int w = 0; w < 2; ++w) {
+                                float one[1];
+                                unpack<1>(raw[y][u][w], one, T{});
+                                x[u][w] = one[0];
+                            }
+                        fetch(job + AHEAD, raw[y]);
+                        float inv = 1.f;
+                        if (weight) {
+                            float ssq = 0.f;
+#pragma unroll
+                            for (int u = 0; u < NI; ++u) ssq = fmaf(x[u][1], x[u][1], fmaf(x[u][0], x[u][0], ssq));
+                            inv = rsqrtf(fmaf(head_sum(ssq, lanes, llanes), a.inv_dim, a.eps));
+                        }
 #pragma unroll
                         for (int u = 0; u < NI; ++u) {
-                            float pu[V], pv[V], t0[V], t1[V], qu[V], qv[V];
-#pragma unroll
-                            for (int c = 0; c < V; ++c) {
-                                pu[c] = INTER ? x[u][2 * c / V][2 * c % V] : x[u][0][c];
-                                pv[c] = INTER ? x[u][(2 * c + 1) / V][(2 * c + 1) % V] : x[u][1][c];
-                            }
-                            if (weight) { vmul<V>(pu, pu, inv); vmul<V>(pv, pv, inv); }
-#pragma unroll
-                            for (int c = 0; c < V; ++c) { qu[c] = pu[c]; qv[c] = pv[c]; }
-                            if (rot < D) {                 // channels that do not turn: their neighbour, whatever it holds, plays no part
-#pragma unroll
-                                for (int c = 0; c < V; ++c) {
-                                    const bool t = turned[u] && (!INTER || (e[u][0] >> 1) + c < pairs);
-                                    qu[c] = t ? qu[c] : 0.f; qv[c] = t ? qv[c] : 0.f;
-                                }
-                            }
-                            vmul<V>(t0, qv, sv[u]);
-                            vmul<V>(t1, qu, su[u]);
-                            vfma<V>(t0, pu, cu[u], t0);
-                            vfma<V>(t1, pv, cv[u], t1);
-                            float r0[V], r1[V];
-#pragma unroll
-                            for (int c = 0; c < V; ++c) {
-                                if (INTER) { (2 * c < V ? r0 : r1)[2 * c % V] = t0[c]; (2 * c + 1 < V ? r0 : r1)[(2 * c + 1) % V] = t1[c]; }
-                                else { r0[c] = t0[c]; r1[c] = t1[c]; }
-                            }
-                            res[u][0] = pack<V>(r0, T{}); res[u][1] = pack<V>(r1, T{});
+                            const float pu = x[u][0] * inv, pv = x[u][1] * inv, qu = turned[u] ? pu : 0.f, qv = turned[u] ? pv : 0.f;
+                            const float r0[1] = {fmaf(pu, cu[u][0], qv * sv[u][0])}, r1[1] = {fmaf(pv, cv[u][0], qu * su[u][0])};
+                            res[u][0] = pack<1>(r0, T{}); res[u][1] = pack<1>(r1, T{});
                         }
                     }
                     if (store && (job + 1 < jobs || last_on)) {
