@@ -367,7 +367,11 @@ static int rotation_of(PyObject* const* a, const Facts* like, ttf_rotation* r, c
         if (r->axes != 1) return 0;
     } else {
         if (!PyTuple_Check(a[6]) || PyTuple_GET_SIZE(a[6]) != r->axes) return 0;
-        for (int i = 0; i < r->axes; ++i) r->section[i] = (int)PyLong_AsLong(PyTuple_GET_ITEM(a[6], i));
+        for (int i = 0; i < r->axes; ++i) {
+            const long section = PyLong_AsLong(PyTuple_GET_ITEM(a[6], i));
+            if (section != (int)section) return 0;
+            r->section[i] = (int)section;
+        }
     }
     r->cyclic = PyObject_IsTrue(a[7]);
     r->factor = (float)PyFloat_AsDouble(a[8]);

@@ -300,3 +300,17 @@ def test_a_process_may_begin_with_a_capture(new, dtype):
     r = subprocess.run([sys.executable, "-c", FIRST.format(new=new, dtype=dtype)], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
                        capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+def test_numbers_beyond_an_int_are_refused():
+    q, out = torch.zeros((4, 2, 8), device="cuda"), torch.zeros((4, 2, 8), device="cuda")
+    pos, freq = torch.zeros((4, 3), device="cuda", dtype=torch.int32), torch.ones(4, device="cuda")
+    P.ttf_rotate(q, None, pos, freq, sections=(2, 1, 1), out_q=out)
+    with pytest.raises((OverflowError, ValueError)):
+        P.ttf_rotate(q, None, pos, freq, sections=(2**32 + 2, 1, 1), out_q=out)
+    with pytest.raises((OverflowError, ValueError)):
+        P.ttf_rotate(q, None, pos, freq, sections=(2, 1, 1), rot_dim=2**32 + 8, out_q=out)
+    b = Batch([1], [3], 16, 2, 1, 8, "f32")
+    q, k, v, st, ln, tb = b.on_device()
+    with pytest.raises((OverflowError, ValueError)):
+        P.ttf_attend(q, k, v, st, ln, tb, 1.0, window=2**32 + 1, out=torch.zeros_like(q))
