@@ -358,12 +358,13 @@ typedef struct {
 /* The sequences of a call.  Rows [start[b], start[b + 1]) of the packed inputs are the new tokens of sequence b (none is
  * allowed); they are the last ones of its length[b] cached tokens, so row i has slot length[b] - start[b + 1] + i.  Slot s
  * lies in page table[b * table_stride + s / page_size], row s % page_size.  All three arrays are device memory and are read
- * by the kernels: lengths may be results of earlier work on the stream (L' of ttf_compress among them).  Rows at or beyond
- * start[seqs] are left as they are.  A sequence whose rows do not lie in [0, rows], whose length is negative, above 2^30 or beyond
- * table_pages pages, and a page that is needed and not in [0, pages), never make a kernel leave its arrays: ttf_paged_status
- * tells TTF_ERR_BOUNDS, and the outputs and new cache rows of that sequence are undefined.  Entries of the table that no
- * slot below length[b] needs may hold anything.  Tokens that lie before the cache (length[b] below the number of new rows)
- * have no slot: they are not stored and see nothing. */
+ * by the kernels: lengths may be results of earlier work on the stream (L' of ttf_compress among them).  Rows before start[0]
+ * and rows at or beyond start[seqs] are left as they are.  A sequence whose rows do not lie in [0, rows] or go back
+ * (start[b + 1] < start[b]), whose length is negative, above 2^30 or beyond table_pages pages (with new rows or without), and a
+ * page that is needed and not in [0, pages), never make a kernel leave its arrays: ttf_paged_status tells TTF_ERR_BOUNDS, and the
+ * outputs and new cache rows of that sequence are undefined, as are those of rows that two sequences claim; all others are as
+ * they should be.  Entries of the table that no slot below length[b] needs may hold anything.  Tokens that lie before the cache
+ * (length[b] below the number of new rows) have no slot: they are not stored and see nothing. */
 typedef struct {
     const int* start;                /* [seqs + 1]                                                                     */
     const int* length;               /* [seqs]                                                                         */

@@ -74,8 +74,22 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
     }
     pdl_wait();
     int n = a.rows;
-    if (APPEND) n = min(n, max(0, __ldcg(a.seq.start + a.seq.seqs)));
-    else if (a.count) n = min(n, max(0, __ldcg(a.count)));
+    if (APPEND) {
+        // rows up to the last one that a sequence within the arrays claims (usually start[seqs]; a start that goes back, or
+        // one outside the arrays, takes no rows from the sequences before it)
+        n = 0;
+        for (int s = ln; s < a.seq.seqs; s += 32) {
+            const int first = __ldcg(a.seq.start + s), end = __ldcg(a.seq.start + s + 1);
+            if (first >= 0 && end > first && end <= a.rows) n = max(n, end);
+        }
+        n = __reduce_max_sync(0xffffffffu, n);
+        // what is wrong with any sequence is reported by the warp that has the least to do
+        if (blockIdx.x == gridDim.x - 1 && warp == kRotThreads / 32 - 1) {
+            bool bad = false;
+            for (int s = ln; s < a.seq.seqs; s += 32) bad |= !seq_range(a.seq, s, a.cache.page).ok;
+            if (bad) report_paged(a.hdr, 2);
+        }
+    } else if (a.count) n = min(n, max(0, __ldcg(a.count)));
 
     const int warps = gridDim.x * (kRotThreads / 32);
     int parts = 1;                                         // of a row's heads
@@ -114,9 +128,25 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
                 b += __popc(__ballot_sync(0xffffffffu, s < a.seq.seqs && __ldcg(a.seq.start + s + 1) <= row));
             SeqRange r = {0, 0, 0, false};
             if (b < a.seq.seqs) r = seq_range(a.seq, b, a.cache.page);
-            const int i = row - r.first, slot = r.length - r.n + i;
-            there = r.ok && i >= 0 && i < r.n;
-            bool bad = !there;
+            there = r.ok && row >= r.first && row - r.first < r.n;
+            if (!there) {                                  // a row of no sequence, or starts that go back somewhere: look at all
+                unsigned found = 0;
+                for (int s0 = 0; s0 < a.seq.seqs && !found; s0 += 32) {
+                    SeqRange c = {0, 0, 0, false};
+                    if (s0 + ln < a.seq.seqs) c = seq_range(a.seq, s0 + ln, a.cache.page);
+                    found = __ballot_sync(0xffffffffu, c.ok && row >= c.first && row - c.first < c.n);
+                    if (found) {
+                        const int src = __ffs(found) - 1;
+                        b = s0 + src;
+                        r.first = __shfl_sync(0xffffffffu, c.first, src);
+                        r.n = __shfl_sync(0xffffffffu, c.n, src);
+                        r.length = __shfl_sync(0xffffffffu, c.length, src);
+                    }
+                }
+                there = found != 0;
+            }
+            const int slot = r.length - r.n + (row - r.first);
+            bool bad = false;
             if (there && slot >= 0) {
                 const int index = quotient(slot, a.cache.page);
                 const long long g = page_of(a.seq.table + (long long)b * a.seq.table_stride, index, a.cache.pages, bad);
