@@ -412,7 +412,9 @@ int ttf_attend(const ttf_heads* q, const ttf_sequences* sequences, const ttf_cac
 /*
  * Device-side status of ttf_rotate, ttf_cache_append and ttf_attend: waits for `stream`, then stores in *host_status the
  * worst of what any of these calls has reported on the current device since the last query, and clears it: TTF_OK,
- * TTF_ERR_TIMEOUT (a kernel gave up on a bounded wait; its outputs are undefined) or TTF_ERR_BOUNDS (see ttf_sequences).
+ * TTF_ERR_TIMEOUT (a kernel gave up on a bounded wait; its outputs are undefined) or TTF_ERR_BOUNDS (see ttf_sequences).  All
+ * streams and host threads of a device share the word, and whoever asks takes what it holds; a report that comes from another
+ * stream meanwhile is told by this query or by the next one.
  */
 int ttf_paged_status(ttf_stream_t stream, int* host_status);
 

@@ -11,7 +11,7 @@ namespace ttf {
 
 // What the calls report stays here until ttf_paged_status asks: one block per device, part of the library image, so that
 // no call needs scratch and a captured graph none that could be given back.
-static __device__ int g_paged_words[kHdrInts];
+static __device__ int g_paged_words[kHdrInts + 1];         // (the last word: what a query has taken)
 constexpr int kMaxDevices = 64;
 static int* g_paged_addr[kMaxDevices] = {};
 static std::mutex g_paged_mu;
@@ -43,6 +43,10 @@ static int begin_paged(int* hdr, cudaStream_t st) {
 #else
 static int begin_paged(int*, cudaStream_t) { return TTF_OK; }
 #endif
+
+// reading and clearing is one step: a report of another stream comes before it, and is told now, or after it, and stays
+__global__ void k_paged_take(int* words) { words[kHdrInts] = atomicExch(words + HDR_ERROR, 0); }
+static std::mutex g_paged_query_mu;                        // one query at a time: they share the word
 
 struct Range { Range(const char* name) { nvtxRangePushA(name); } ~Range() { nvtxRangePop(); } };
 
@@ -192,11 +196,18 @@ int ttf_paged_status(ttf_stream_t stream, int* host_status) {
     if (!host_status) return TTF_ERR_INVALID_ARG;
     int* words = nullptr;
     TTF_CHECK(paged_words(&words));
-    cudaError_t e = cudaStreamSynchronize((cudaStream_t)stream);
+    const cudaStream_t st = (cudaStream_t)stream;
+    cudaError_t e = cudaStreamSynchronize(st);             // (the caller's work, which may be long, without the lock)
     if (e != cudaSuccess) return cuda_fail(e);
     int v = 0;
-    e = cudaMemcpy(&v, words + HDR_ERROR, sizeof(int), cudaMemcpyDeviceToHost);
-    if (e == cudaSuccess && v) e = cudaMemset(words + HDR_ERROR, 0, sizeof(int));
+    {
+        std::lock_guard<std::mutex> lk(g_paged_query_mu);
+        k_paged_take<<<1, 1, 0, st>>>(words);
+        e = cudaGetLastError();
+        if (e == cudaSuccess) e = cudaMemcpyAsync(&v, words + kHdrInts, sizeof(int), cudaMemcpyDeviceToHost, st);
+        const cudaError_t w = cudaStreamSynchronize(st);   // (in any case: nothing may write v when it is gone)
+        if (e == cudaSuccess) e = w;
+    }
     if (e != cudaSuccess) return cuda_fail(e);
     *host_status = v == 0 ? TTF_OK : (v == 2 ? TTF_ERR_BOUNDS : TTF_ERR_TIMEOUT);
     return TTF_OK;
