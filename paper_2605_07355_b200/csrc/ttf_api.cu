@@ -37,7 +37,9 @@ int sm_count() {
     return n;
 }
 
-// ---- per-(function, device) record of the dynamic shared memory limit that has been set ------------------
+// ---- per-(function, device) record of an attribute that has been set (the size of the dynamic shared memory, ...) --------
+// The lock is held until the attribute is set: a second host thread whose first call comes at the same time must not launch
+// before that.
 struct FuncAttrTable {
     std::mutex mu;
     std::map<std::pair<const void*, int>, size_t> set;
@@ -49,32 +51,28 @@ struct FuncAttrTable {
         have = bytes;
         return true;
     }
-    void forget(const void* func, int dev) {
+    // sets the attribute of `func` on the current device to `value`, unless it is that large already
+    cudaError_t ensure(const void* func, cudaFuncAttribute attr, size_t value) {
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
         std::lock_guard<std::mutex> lk(mu);
-        set.erase(std::make_pair(func, dev));
+        size_t& have = set[std::make_pair(func, dev)];
+        if (have >= value) return cudaSuccess;
+        e = cudaFuncSetAttribute(func, attr, (int)value);
+        if (e == cudaSuccess) have = value;
+        return e;
     }
 };
 static FuncAttrTable g_func_attr;
 
 cudaError_t ensure_dynamic_smem(const void* func, size_t bytes) {
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (!g_func_attr.needs(func, dev, bytes)) return cudaSuccess;
-    e = cudaFuncSetAttribute(func, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (e != cudaSuccess) g_func_attr.forget(func, dev);
-    return e;
+    return g_func_attr.ensure(func, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
 cudaError_t allow_large_cluster(const void* func) {
     static FuncAttrTable allowed;
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (!allowed.needs(func, dev, 1)) return cudaSuccess;
-    e = cudaFuncSetAttribute(func, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e != cudaSuccess) allowed.forget(func, dev);
-    return e;
+    return allowed.ensure(func, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
 }
 
 static std::atomic<int> g_wait_limit{1 << 18};
