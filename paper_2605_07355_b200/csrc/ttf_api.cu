@@ -70,9 +70,27 @@ cudaError_t ensure_dynamic_smem(const void* func, size_t bytes) {
     return g_func_attr.ensure(func, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
-cudaError_t allow_large_cluster(const void* func) {
-    static FuncAttrTable allowed;
-    return allowed.ensure(func, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+bool large_cluster_fits(const void* func, int threads, size_t smem) {
+    static std::mutex mu;
+    static std::map<std::pair<const void*, int>, bool> known;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    std::lock_guard<std::mutex> lk(mu);
+    const auto key = std::make_pair(func, dev);
+    const auto it = known.find(key);
+    if (it != known.end()) return it->second;
+    int n = 0;
+    if (cudaFuncSetAttribute(func, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(16); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = 16; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr; cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&n, func, &cfg) != cudaSuccess) n = 0;
+    }
+    if (n < 1) cudaGetLastError();                         // (a refusal is an answer here, not an error of the call)
+    return known[key] = n > 0;
 }
 
 static std::atomic<int> g_wait_limit{1 << 18};

@@ -270,6 +270,7 @@ template <int DP, int STAGES> static cudaError_t launch_few_t(const AttendArgs& 
     const size_t smem = S::SMEM + 1024;
     cudaError_t e = ensure_dynamic_smem(fn, smem);
     if (e != cudaSuccess) return e;
+    if (ls > 3 && !large_cluster_fits(fn, kMmaThreads, smem)) ls = 3;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(ctas << ls)); cfg.blockDim = dim3(kMmaThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -278,10 +279,6 @@ template <int DP, int STAGES> static cudaError_t launch_few_t(const AttendArgs& 
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = 1u << ls; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = ls ? 2 : 1;
-    if (ls > 3) {                                          // (clusters of 16 have to be asked for)
-        e = allow_large_cluster(fn);
-        if (e != cudaSuccess) return e;
-    }
     return cudaLaunchKernelEx(&cfg, k_attend_few<DP, STAGES>, maps, a, ls);
 }
 cudaError_t launch_attend_few(const AttendArgs& a, cudaStream_t st) {

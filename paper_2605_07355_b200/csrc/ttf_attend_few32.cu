@@ -253,7 +253,8 @@ template <int VN> static cudaError_t launch_few32_t(const AttendArgs& a, cudaStr
     cudaError_t e = ensure_dynamic_smem(fn, smem);
     if (e != cudaSuccess) return e;
     const long long ctas = most_tiles(a, kF32Rows, 0) * a.cache.heads;
-    const int ls = few_split(a, ctas);
+    int ls = few_split(a, ctas);
+    if (ls > 3 && !large_cluster_fits(fn, kMmaThreads, smem)) ls = 3;
     if ((ctas << ls) > 0x7fffffffLL) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(ctas << ls)); cfg.blockDim = dim3(kMmaThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
@@ -263,10 +264,6 @@ template <int VN> static cudaError_t launch_few32_t(const AttendArgs& a, cudaStr
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = 1u << ls; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = ls ? 2 : 1;
-    if (ls > 3) {                                          // (clusters of 16 have to be asked for)
-        e = allow_large_cluster(fn);
-        if (e != cudaSuccess) return e;
-    }
     return cudaLaunchKernelEx(&cfg, k_attend_few32<VN>, a, ls);
 }
 cudaError_t launch_attend_few32(const AttendArgs& a, cudaStream_t st) {

@@ -295,7 +295,8 @@ template <int DC, bool PAGE16, bool FULL> static cudaError_t launch_mma_f(const 
     cudaError_t e = ensure_dynamic_smem(fn, smem);
     if (e != cudaSuccess) return e;
     const long long ctas = most_tiles(a, kMmaRows, 0) * a.cache.heads;
-    const int ls = few_split(a, ctas);
+    int ls = few_split(a, ctas);
+    if (ls > 3 && !large_cluster_fits(fn, kMmaThreads, smem)) ls = 3;
     if ((ctas << ls) > 0x7fffffffLL) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(ctas << ls)); cfg.blockDim = dim3(kMmaThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
@@ -305,10 +306,6 @@ template <int DC, bool PAGE16, bool FULL> static cudaError_t launch_mma_f(const 
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = 1u << ls; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = ls ? 2 : 1;
-    if (ls > 3) {                                          // (clusters of 16 have to be asked for)
-        e = allow_large_cluster(fn);
-        if (e != cudaSuccess) return e;
-    }
     return cudaLaunchKernelEx(&cfg, k_attend_mma<DC, PAGE16, FULL>, a, ls);
 }
 template <int DC, bool PAGE16> static cudaError_t launch_mma_t(const AttendArgs& a, cudaStream_t st) {

@@ -185,7 +185,9 @@ int sm_count();   // SMs of the current device (cached per device)
 // cudaFuncAttributeMaxDynamicSharedMemorySize belongs to a function in the context of ONE device: set it the first
 // time `func` is launched on the current device (and again if a larger size is asked for).
 cudaError_t ensure_dynamic_smem(const void* func, size_t bytes);
-cudaError_t allow_large_cluster(const void* func);         // the same for clusters of more than eight CTAs
+// Clusters of sixteen CTAs have to be asked for, and the device has to have one GPC with room for all of them: true when `func`
+// may be launched in such clusters on the current device (asked once; ensure_dynamic_smem comes before it).
+bool large_cluster_fits(const void* func, int threads, size_t smem);
 
 // Bounded waits: polls of an mbarrier before a waiter gives up, and extra bytes announced to it (always 0 outside
 // the test that makes a wait run out; see ttf_debug_set_wait).
