@@ -219,6 +219,7 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
         return false;
     };
 
+    int issued = 0, raw_at = -1;                           // warp 8: ring slots filled so far; phase of bar_raw that has not come
     if (warp == 8) {
         // ---- producer -------------------------------------------------------------------------------------------
         bool bad = false;
@@ -231,7 +232,7 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
         }
         const int* const table = a.seq.table + (long long)t.seq * a.seq.table_stride;
         const int page = (int)a.cache.page.d;
-        int issued = 0, raw = 0;
+        int raw = 0;
         auto page_id = [&](int j) {                        // lane = page of the block (box_rows rows each)
             const int s0 = j * block + lane * box_rows;
             if (lane * box_rows >= block || j >= j_hi || s0 >= hi_u || s0 + box_rows <= lo_u) return -1;
@@ -262,8 +263,10 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
                 }
                 issued = idx + 1;
                 if (kv && edge) {                          // their values: zeros, whatever the page (or an earlier block) holds
-                    ok = __all_sync(0xffffffffu, wait(&bar_raw, raw & 1));
+                    raw_at = raw & 1;
+                    ok = __all_sync(0xffffffffu, wait(&bar_raw, raw_at));
                     if (!ok) break;
+                    raw_at = -1;
                     ++raw;
                     const int head = max(0, lo_u - s0) * 8, tail = max(0, hi_u - s0) * 8;      // in 16-byte pieces
 #pragma unroll
@@ -280,12 +283,6 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
             id = next;
         }
         if (__any_sync(0xffffffffu, bad) && lane == 0) report_paged(a.hdr, 2);
-        if (failed()) {                                    // copies in flight land before the CTA may leave
-            if (j_lo < j_hi) mbar_wait(&bar_q, 0, limit);
-            mbar_wait(&bar_raw, raw & 1, limit);
-            for (int i = issued > S::RING ? issued - S::RING : 0; i < issued; ++i)
-                mbar_wait(&bar_full[i % S::RING], (i / S::RING) & 1, limit);
-        }
     } else if (warp >= 9) {
         // ---- products: one thread per tile ------------------------------------------------------------------------
         if (lane == 0) {
@@ -521,7 +518,13 @@ k_attend_tc(const __grid_constant__ AttendMaps maps, const __grid_constant__ Att
         }
     }
     tc_fence_before();
-    __syncthreads();
+    __syncthreads();                                       // (from here on nobody gives up any more)
+    if (warp == 8 && s_err) {                              // copies in flight land before the CTA may leave
+        if (j_lo < j_hi) mbar_wait(&bar_q, 0, limit);
+        if (raw_at >= 0) { mbar_wait(&bar_raw, raw_at, limit); --issued; }           // (that slot is never declared full)
+        for (int i = issued > S::RING ? issued - S::RING : 0; i < issued; ++i)
+            mbar_wait(&bar_full[i % S::RING], (i / S::RING) & 1, limit);
+    }
     if (warp == 9) {
         tc_fence_after();
         if (s_err) mbar_wait(&bar_end, 0, limit);          // products in flight end before their accumulators are given back
