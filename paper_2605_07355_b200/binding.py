@@ -225,6 +225,27 @@ def _stream_of(x: torch.Tensor, stream) -> int:
     return _current_raw_stream(x.get_device()) if stream is None else _stream_ptr(stream)
 
 
+def _fresh(like: torch.Tensor, shape, dtype, stream) -> torch.Tensor:
+    """A new tensor that is written on `stream`.  Where that is not the current stream, memory that was freed on the current one
+    may still be in use there: the tensor then comes from `stream`'s own memory, and is held for the current stream, on which the
+    caller goes on with it."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    address, here = _stream_ptr(stream), torch.cuda.current_stream(like.device)
+    if address == here.cuda_stream:
+        return like.new_empty(shape, dtype=dtype)
+    if isinstance(stream, torch.cuda.Stream):
+        on = stream
+    elif address <= 1:                                     # (0 and cudaStreamLegacy)
+        on = torch.cuda.default_stream(like.device)
+    else:
+        on = torch.cuda.ExternalStream(address, like.device)
+    with torch.cuda.stream(on):
+        out = like.new_empty(shape, dtype=dtype)
+    out.record_stream(here)
+    return out
+
+
 def _check_operands(name: str, first: torch.Tensor, *others) -> None:
     """The first tensor of an entry point without _check_features decides the device, so it must be on one; the others must
     be memory a kernel can read (a NULL is the library's to refuse)."""
@@ -265,11 +286,11 @@ def ttf_compress(features: torch.Tensor, r: int, t: float, out_tokens: Optional[
                                 anchor_frame, order, pos_base)
     n = F * H * W
     if out_tokens is None:
-        out_tokens = features.new_empty((n, C))
+        out_tokens = _fresh(features, (n, C), features.dtype, stream)
     if out_count is None:
-        out_count = features.new_empty(1, dtype=torch.int32)
+        out_count = _fresh(features, 1, torch.int32, stream)
     if out_pos_thw is None:
-        out_pos_thw = features.new_empty((n, 3), dtype=torch.int32)
+        out_pos_thw = _fresh(features, (n, 3), torch.int32, stream)
     fast, sp, dt = _fast or _marshal(), _stream_of(features, stream), _dtype_code(features)
     if workspace is None:
         rc = fast.compress(features.data_ptr(), F, H, W, C, int(r), float(t), dt, int(anchor_mode), int(anchor_frame),
@@ -377,9 +398,9 @@ def ttf_compress_mean(features: torch.Tensor, r: int, t: float, stream=None):
     F, H, W, C = _check_features(features, "cuda")
     dev = features.device
     n = F * H * W
-    out_tokens = torch.empty((n, C), dtype=features.dtype, device=dev)
-    out_count = torch.empty(1, dtype=torch.int32, device=dev)
-    out_pos_thw = torch.empty((n, 3), dtype=torch.int32, device=dev)
+    out_tokens = _fresh(features, (n, C), features.dtype, stream)
+    out_count = _fresh(features, 1, torch.int32, stream)
+    out_pos_thw = _fresh(features, (n, 3), torch.int32, stream)
     with torch.cuda.device(dev):
         rc = lib().ttf_compress_mean(_p(features), F, H, W, C, int(r), float(t), _dtype_code(features),
                                      _p(out_tokens), _p(out_count), _p(out_pos_thw), _stream_ptr(stream))
@@ -410,11 +431,11 @@ def ttf_compress_batch(features, r: int, t: float, out_tokens=None, out_count=No
     F, H, W, C = shape
     n, B = F * H * W, len(feats)
     if out_tokens is None:
-        out_tokens = [first.new_empty((n, C)) for _ in range(B)]
+        out_tokens = [_fresh(first, (n, C), dt, stream) for _ in range(B)]
     if out_count is None:
-        out_count = [first.new_empty(1, dtype=torch.int32) for _ in range(B)]
+        out_count = [_fresh(first, 1, torch.int32, stream) for _ in range(B)]
     if out_pos_thw is None:
-        out_pos_thw = [first.new_empty((n, 3), dtype=torch.int32) for _ in range(B)]
+        out_pos_thw = [_fresh(first, (n, 3), torch.int32, stream) for _ in range(B)]
     if not (len(out_tokens) == len(out_count) == len(out_pos_thw) == B):
         raise ValueError("one output of each kind per clip")
     rc = (_fast or _marshal()).compress_batch(
@@ -438,15 +459,15 @@ def ttf_query(features: torch.Tensor, r: int, t: float, workspace: Optional[torc
     n = F * H * W
     out = {}
     if "anchor" in want:
-        out["anchor"] = features.new_empty(1, dtype=torch.int32)
+        out["anchor"] = _fresh(features, 1, torch.int32, stream)
     if "keep" in want:
-        out["keep"] = features.new_empty(n, dtype=torch.uint8)
+        out["keep"] = _fresh(features, n, torch.uint8, stream)
     if "dst" in want:
-        out["dst"] = features.new_empty(n, dtype=torch.int32)
+        out["dst"] = _fresh(features, n, torch.int32, stream)
     if "best_sim" in want:
-        out["best_sim"] = features.new_empty(n, dtype=torch.float32)
+        out["best_sim"] = _fresh(features, n, torch.float32, stream)
     if "fuse_cnt" in want:
-        out["fuse_cnt"] = features.new_empty(H * W, dtype=torch.int32)
+        out["fuse_cnt"] = _fresh(features, H * W, torch.int32, stream)
     outs = [_addr(out.get(k)) for k in ("anchor", "keep", "dst", "best_sim", "fuse_cnt")]
     fast, sp, dt = _fast or _marshal(), _stream_of(features, stream), _dtype_code(features)
     if workspace is None:
@@ -488,9 +509,9 @@ def ttf_compress_segment(features: torch.Tensor, r: int, t: float, frame_base: i
         with there:
             return ttf_compress_segment(features, r, t, frame_base, stream)
     n = max(1, (F - 1) * H * W)
-    out_tokens = features.new_empty((n, C))
-    out_count = features.new_empty(1, dtype=torch.int32)
-    out_pos = features.new_empty((n, 3), dtype=torch.int32)
+    out_tokens = _fresh(features, (n, C), features.dtype, stream)
+    out_count = _fresh(features, 1, torch.int32, stream)
+    out_pos = _fresh(features, (n, 3), torch.int32, stream)
     rc = (_fast or _marshal()).compress_segment(features.data_ptr(), F, H, W, C, int(r), float(t), _dtype_code(features),
                                                 int(frame_base), out_tokens.data_ptr(), out_count.data_ptr(),
                                                 out_pos.data_ptr(), _stream_of(features, stream))
@@ -512,8 +533,8 @@ def ttf_restore(compressed: torch.Tensor, F: int, H: int, W: int, anchor: torch.
     if compressed.shape[0] == 0:
         raise IndexError("compressed has no rows")
     row_bytes = compressed.numel() // compressed.shape[0] * compressed.element_size()
-    out = compressed.new_empty((F * H * W,) + tuple(compressed.shape[1:]))
-    idx = compressed.new_empty(F * H * W, dtype=torch.int32)
+    out = _fresh(compressed, (F * H * W,) + tuple(compressed.shape[1:]), compressed.dtype, stream)
+    idx = _fresh(compressed, F * H * W, torch.int32, stream)
     rc = (_fast or _marshal()).restore(compressed.data_ptr(), row_bytes, F, H, W, _addr(anchor), _addr(keep),
                                        _addr(dst), out.data_ptr(), idx.data_ptr(), _stream_of(compressed, stream))
     if rc != TTF_OK:
@@ -524,7 +545,7 @@ def ttf_restore(compressed: torch.Tensor, F: int, H: int, W: int, anchor: torch.
 def ttf_sim_histogram(best_sim: torch.Tensor, anchor: torch.Tensor, F: int, H: int, W: int, bins: int, stream=None):
     """ttf_sim_histogram: uint32 counts [bins] (returned as an int32 tensor with the same bits)."""
     dev = best_sim.device
-    hist = torch.empty(bins, dtype=torch.int32, device=dev)
+    hist = _fresh(best_sim, bins, torch.int32, stream)
     with torch.cuda.device(dev):
         rc = lib().ttf_sim_histogram(_p(best_sim), _p(anchor), F, H, W, int(bins), _p(hist), _stream_ptr(stream))
     if rc != TTF_OK:
@@ -540,7 +561,7 @@ def ttf_stats(best_sim: torch.Tensor, keep: torch.Tensor, anchor: torch.Tensor, 
     if there is not None:
         with there:
             return ttf_stats(best_sim, keep, anchor, F, H, W, t, band, stream)
-    out = best_sim.new_empty(3, dtype=torch.int64)
+    out = _fresh(best_sim, 3, torch.int64, stream)
     rc = (_fast or _marshal()).stats(best_sim.data_ptr(), _addr(keep), _addr(anchor), F, H, W, float(t),
                                      float(band), out.data_ptr(), _stream_of(best_sim, stream))
     if rc != TTF_OK:
@@ -620,10 +641,10 @@ def _heads(name: str, x: Optional[torch.Tensor], like: torch.Tensor):
     return x.data_ptr(), row, head, shape[1]
 
 
-def _out_heads(name: str, out: Optional[torch.Tensor], x: torch.Tensor, like: torch.Tensor):
+def _out_heads(name: str, out: Optional[torch.Tensor], x: torch.Tensor, like: torch.Tensor, stream):
     """the output that goes with x: as given, or new"""
     if out is None:
-        out = x.new_empty(x.shape)
+        out = _fresh(x, x.shape, x.dtype, stream)
     elif out.shape != x.shape:
         raise ValueError(f"{name} must have the shape of its input, {tuple(x.shape)}, got {tuple(out.shape)}")
     return out, _heads(name, out, like)
@@ -696,11 +717,11 @@ def ttf_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: 
     qh, kh = _heads("q", q, like), _heads("k", k, like)
     oq = ok = _NO_HEADS
     if q is not None:
-        out_q, oq = _out_heads("out_q", out_q, q, like)
+        out_q, oq = _out_heads("out_q", out_q, q, like, stream)
     elif out_q is not None:
         raise ValueError("out_q without q")
     if k is not None:
-        out_k, ok = _out_heads("out_k", out_k, k, like)
+        out_k, ok = _out_heads("out_k", out_k, k, like, stream)
     elif out_k is not None:
         raise ValueError("out_k without k")
     pos, rotation = _rotation(positions, freq, q_weight, k_weight, rot_dim, interleaved, sections, cyclic, factor, eps, like)
@@ -767,7 +788,7 @@ def ttf_cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_
                                     sections=sections, cyclic=cyclic, factor=factor, stream=stream)
     kh, vh, qh, oq = _heads("k", k, k), _heads("v", v, k), _heads("q", q, k), _NO_HEADS
     if q is not None:
-        out_q, oq = _out_heads("out_q", out_q, q, k)
+        out_q, oq = _out_heads("out_q", out_q, q, k, stream)
     elif out_q is not None:
         raise ValueError("out_q without q")
     if (positions is None) != (freq is None):
@@ -808,7 +829,7 @@ def ttf_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, st
             return ttf_attend(q, k_cache, v_cache, start, length, table, scale, causal=causal, window=window, out=out,
                               stream=stream)
     qh = _heads("q", q, q)
-    out, oh = _out_heads("out", out, q, q)
+    out, oh = _out_heads("out", out, q, q, stream)
     cache, sequences = _cache(k_cache, v_cache, q), _sequences(start, length, table, q)
     if q.shape[0] == 0:
         return out
