@@ -52,7 +52,8 @@ struct RotateArgs {
     int dim, rows;
     const int* count;
     const int* pos;
-    const float* freq;                             // NULL: no rotation and no norm (append of keys as they come)
+    const float* freq;
+    bool as_they_come;                             // append: keys are copied
     int rot, interleaved, axes, sec1, sec2, sec0, cyclic;
     float factor, eps, inv_dim;
     const void *q_weight, *k_weight;

@@ -167,6 +167,7 @@ int ttf_cache_append(const ttf_heads* k, const ttf_heads* v, const ttf_heads* q,
     a.q = ttf::view(q, rows); a.k = ttf::view(k, rows); a.v = ttf::view(v, rows); a.out_q = ttf::view(out_q, rows);
     a.dim = cache->head_dim; a.inv_dim = 1.f / cache->head_dim; a.rows = sequences->rows;
     take_rotation(rotation, positions, &a);
+    a.as_they_come = !rotation || (!rotation->k_weight && rotation->rot_dim == 0);
     a.seq = ttf::view(sequences); a.cache = ttf::view(cache);
     Range range("ttf cache append");
     TTF_CHECK(begin_paged(a.hdr, (cudaStream_t)stream));

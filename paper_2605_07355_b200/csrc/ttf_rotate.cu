@@ -158,6 +158,7 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
             if (bad && ln == 0) report_paged(a.hdr, 2);
         };
 
+        // kinds: 0 queries, 1 keys, 2 what is copied bit for bit: values, keys as they come
         auto pass = [&](auto kind_of, const HeadsView& src_of, int first, const void* weight, T* to, long long to_head, bool store) {
             constexpr int KIND = decltype(kind_of)::value;
             const int b = max(h0, first), z = min(h1, first + src_of.heads);
@@ -187,7 +188,7 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
             have = true;
             if (APPEND) {
                 store = store && (KIND == 0 ? there : stored);
-                to += KIND == 0 ? 0 : (KIND == 1 ? k_at : v_at);
+                to += KIND == 0 ? 0 : (KIND == 1 || first == Hq ? k_at : v_at);
             }
             to += (long long)(b - first + sub) * to_head;
             const long long to_step = to_head << (5 - llanes);
@@ -336,8 +337,12 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
         };
         pass(std::integral_constant<int, 0>{}, a.q, 0, a.q_weight, reinterpret_cast<T*>(a.out_q.data) + (long long)row * a.out_q.row, a.out_q.head, true);
         if (APPEND) {
-            pass(std::integral_constant<int, 1>{}, a.k, Hq, a.k_weight, reinterpret_cast<T*>(a.cache.k), a.cache.k_head, true);
-            pass(std::integral_constant<int, 2>{}, a.v, Hq + Hk, nullptr, reinterpret_cast<T*>(a.cache.v), a.cache.v_head, true);
+            if (!a.as_they_come)
+                pass(std::integral_constant<int, 1>{}, a.k, Hq, a.k_weight, reinterpret_cast<T*>(a.cache.k), a.cache.k_head, true);
+#pragma unroll 1
+            for (int v = a.as_they_come ? 0 : 1; v < 2; ++v)
+                pass(std::integral_constant<int, 2>{}, v ? a.v : a.k, v ? Hq + Hk : Hq, nullptr, reinterpret_cast<T*>(v ? a.cache.v : a.cache.k),
+                     v ? a.cache.v_head : a.cache.k_head, true);
         } else
             pass(std::integral_constant<int, 1>{}, a.k, Hq, a.k_weight, reinterpret_cast<T*>(a.out_k.data) + (long long)row * a.out_k.row, a.out_k.head, true);
     }
