@@ -210,9 +210,11 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
                         const float wu = INTER ? (2 * c < V ? w0[2 * c % V] : w1[2 * c % V]) : w0[c];
                         const float wv = INTER ? (2 * c + 1 < V ? w0[(2 * c + 1) % V] : w1[(2 * c + 1) % V]) : w1[c];
                         const int j = (INTER ? e[u][0] >> 1 : e[u][0]) + c;
-                        const float2 t = turned[u] && j < pairs ? turn[j] : make_float2(1.f, 0.f);
-                        cu[u][c] = wu * t.x; su[u][c] = wu * t.y;
-                        cv[u][c] = wv * t.x; sv[u][c] = -wv * t.y;
+                        // (channels that do not turn add (+0)(-0) = -0, which changes nothing, a negative zero neither)
+                        const bool on = turned[u] && j < pairs;
+                        const float2 t = on ? turn[j] : make_float2(1.f, 0.f);
+                        cu[u][c] = wu * t.x; su[u][c] = on ? wu * t.y : -0.f;
+                        cv[u][c] = wv * t.x; sv[u][c] = on ? -wv * t.y : -0.f;
                     }
                 }
             }
