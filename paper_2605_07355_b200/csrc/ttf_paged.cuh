@@ -226,7 +226,7 @@ struct Cut { Divisor tokens; int lrows; };         // tiles of `tokens` tokens, 
 inline Cut cut_tokens(int per) { return Cut{make_divisor(per), 0}; }
 inline Cut cut_rows(int lrows) { return Cut{Divisor{0, 0, 0}, lrows}; }
 __device__ __forceinline__ int tiles_of(int n, int group, const Cut& cut) {
-    return cut.tokens.d ? quotient(n + (int)cut.tokens.d - 1, cut.tokens)
+    return cut.tokens.d ? (n > 0 ? quotient(n - 1, cut.tokens) + 1 : 0)
                         : (int)(((long long)n * group + (1 << cut.lrows) - 1) >> cut.lrows);
 }
 __device__ __forceinline__ bool find_tile(const AttendArgs& a, const Cut& cut, int index, bool report, Tile& t) {

@@ -95,8 +95,9 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
     int parts = 1;                                         // of a row's heads
     if (n > 0 && n < warps) parts = min(min(warps / n, (heads + per_warp - 1) / per_warp), kRotParts);
     const int units = n * parts;
-    for (int unit = warp * gridDim.x + blockIdx.x; unit < units; unit += warps) {
-        const int row = parts > 1 ? unit / parts : unit, part = unit - row * parts;
+    // (without a sign: units may be as many as 2^31 - 1, and a warp counts one step beyond them)
+    for (unsigned at = warp * gridDim.x + blockIdx.x; at < (unsigned)units; at += warps) {
+        const int unit = (int)at, row = parts > 1 ? unit / parts : unit, part = unit - row * parts;
         const int h0 = parts > 1 ? heads * part / parts : 0, h1 = parts > 1 ? heads * (part + 1) / parts : heads;
 
         bool have = false;
