@@ -369,7 +369,7 @@ typedef struct {
     const int* start;                /* [seqs + 1]                                                                     */
     const int* length;               /* [seqs]                                                                         */
     const int* table;                /* [seqs, table_pages]                                                            */
-    long long table_stride;          /* elements between the rows of the table                                         */
+    long long table_stride;          /* elements between the rows of the table: table_pages or more, or 0 (one for all) */
     int table_pages;
     int seqs;
     int rows;                        /* capacity of the packed arrays                                                  */
