@@ -726,6 +726,8 @@ def ttf_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: 
         raise ValueError("out_k without k")
     pos, rotation = _rotation(positions, freq, q_weight, k_weight, rot_dim, interleaved, sections, cyclic, factor, eps, like)
     rows, _, dim = like.shape
+    if count is not None and count.numel() != 1:           # (one of no values would read as "all rows")
+        raise ValueError(f"count must be one value, got {count.numel()}")
     cnt = 0 if count is None else _ints("count", count.reshape(-1), 1, like)
     if rows == 0:
         return out_q, out_k
