@@ -55,6 +55,7 @@ template <int DP> struct AttendShape {
     static constexpr int SMEM = 2 * TILE + RING * TILE;
     static constexpr int ML = 2 * kAtRows * DP;                    // what ranks send: [rank][tile][channel][row], then maxima, sums
     static constexpr uint32_t O_COL = 256;                         // tensor memory: S0 0, S1 128, O0, O1 from 256 on
+    static_assert(SMEM + kMatchSmem > kSmShared && 2 * SMEM > kSmShared, "no other CTA with tensor memory fits beside this one");
 };
 
 struct AttendMaps { CUtensorMap q, k, v; };

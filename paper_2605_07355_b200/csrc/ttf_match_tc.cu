@@ -628,7 +628,8 @@ static cudaError_t launch_tc_t(const Problem& p, const TcPlan& plan, const Scrat
             !make_tensor_map(&maps.b[n], p.xs.X[n], 1, p.F, p.H, p.W, p.C, kTcKC, S::BW, S::BH, 1, true))
             return cudaErrorInvalidValue;
     // (at least 80 KB: never three CTAs on one SM while others have one or none; r = 0 would fit three)
-    const size_t need = (size_t)S::RING + S::XBYTES + S::NORMBYTES + 1024, smem = need < 80 * 1024 ? 80 * 1024 : need;
+    const size_t need = (size_t)S::RING + S::XBYTES + S::NORMBYTES + 1024, smem = need < kMatchSmem ? kMatchSmem : need;
+    static_assert(3 * kMatchSmem > kSmShared && S::OWNCH * S::NB <= 256, "tensor memory for all CTAs that an SM takes");
     cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k_match_tc<R, WY, G>), smem);
     if (e != cudaSuccess) return e;
     const long long tiles = plan.tiles;

@@ -5,6 +5,13 @@
 
 namespace ttf {
 
+// Who may be on an SM together.  A CTA holds its columns of tensor memory while it waits at its cluster's barrier, and one that
+// finds too few of them free waits in its allocation: CTAs of two clusters that block one another so would wait for good.  Two
+// CTAs of the matching kernel share an SM with 256 columns each; the attention takes all 512, so neither a second CTA of it nor
+// one of the matching kernel may find room on its SM.  Shared memory sees to that, and the sizes are checked where they are made.
+constexpr int kSmShared = 228 * 1024;              // bytes an SM has for all its CTAs
+constexpr int kMatchSmem = 80 * 1024;              // a CTA of the matching kernel asks for at least so much
+
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
