@@ -398,7 +398,8 @@ int ttf_cache_append(const ttf_heads* k, const ttf_heads* v, const ttf_heads* q,
 /*
  * Attention of the new rows over the cache, which holds their own keys and values already (ttf_cache_append first):
  *   out[i, h] = sum over the visible slots s of softmax_s(scale * <q[i, h], k[s, h / group]>) v[s, h / group]
- * with group = q->heads / cache->heads (a whole number).  Row i at slot c sees every slot of its sequence with causal = 0,
+ * with group = q->heads / cache->heads (a whole number) and scale log2(e) a finite number.  Row i at slot c sees every slot of its
+ * sequence with causal = 0,
  * the slots up to c with causal = 1, of these only those above c - window where window > 0.  A row that sees nothing is
  * zero.  Slots that no row of the sequence sees may hold anything, NaN included.  A value that is infinite or NaN in a slot
  * that some row sees always reaches those rows; in bf16 it may make rows of the same sequence NaN that do not see the slot

@@ -178,7 +178,8 @@ int ttf_cache_append(const ttf_heads* k, const ttf_heads* v, const ttf_heads* q,
 
 int ttf_attend(const ttf_heads* q, const ttf_sequences* sequences, const ttf_cache* cache, float scale, int causal,
                int window, const ttf_heads* out, ttf_stream_t stream) {
-    if (!q || !out || !std::isfinite(scale) || causal < 0 || causal > 1 || window < 0) return TTF_ERR_INVALID_ARG;
+    // (the kernels work in powers of two: scale log2(e) has to be a number as well)
+    if (!q || !out || !std::isfinite(scale * 1.4426950408889634f) || causal < 0 || causal > 1 || window < 0) return TTF_ERR_INVALID_ARG;
     TTF_CHECK(check_cache(cache));
     TTF_CHECK(check_sequences(sequences));
     for (const ttf_heads* h : {q, out}) TTF_CHECK(check_heads(h, sequences->rows));
