@@ -187,6 +187,9 @@ template <int V> __device__ __forceinline__ void unpack_pairs(const typename Vec
 // a call's outputs are not what was asked for: kind 1 a bounded wait gave up, 2 lengths or pages outside their arrays
 __device__ __forceinline__ void report_paged(int* hdr, int kind) { atomicMax(hdr + HDR_ERROR, kind); }
 
+__device__ __forceinline__ bool length_fits(const SeqView& s, int length, const Divisor& page) {
+    return length >= 0 && length <= (1 << 30) && (long long)length <= (long long)s.table_pages * page.d;
+}
 // One sequence of a call, with nothing that could lead out of an array: n new rows from `first` on, `length` slots.
 struct SeqRange { int first, n, length; bool ok; };
 __device__ __forceinline__ SeqRange seq_range(const SeqView& s, int b, const Divisor& page) {
@@ -194,8 +197,7 @@ __device__ __forceinline__ SeqRange seq_range(const SeqView& s, int b, const Div
     r.first = __ldcg(s.start + b);
     const int end = __ldcg(s.start + b + 1);
     r.length = __ldcg(s.length + b);
-    r.ok = r.first >= 0 && end >= r.first && end <= s.rows && r.length >= 0 && r.length <= (1 << 30) &&
-           (long long)r.length <= (long long)s.table_pages * page.d;
+    r.ok = r.first >= 0 && end >= r.first && end <= s.rows && length_fits(s, r.length, page);
     r.n = r.ok ? end - r.first : 0;
     return r;
 }

@@ -74,13 +74,22 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
     }
     pdl_wait();
     int n = a.rows;
+    // append: the rows [first, end) that sequence s claims (none, if they do not lie within the arrays)
+    auto claim = [&](int s, int& first, int& end) {
+        const int f = __ldcg(a.seq.start + s), e = __ldcg(a.seq.start + s + 1);
+        const bool in_rows = f >= 0 && e > f && e <= a.rows;
+        first = in_rows ? f : 0; end = in_rows ? e : 0;
+    };
+    [[maybe_unused]] int first0 = 0, end0 = 0;             // those of this lane's one of the first 32 sequences
     if (APPEND) {
-        // rows up to the last one that a sequence within the arrays claims (usually start[seqs]; a start that goes back, or
-        // one outside the arrays, takes no rows from the sequences before it)
-        n = 0;
-        for (int s = ln; s < a.seq.seqs; s += 32) {
-            const int first = __ldcg(a.seq.start + s), end = __ldcg(a.seq.start + s + 1);
-            if (first >= 0 && end > first && end <= a.rows) n = max(n, end);
+        // rows up to the last one that any sequence claims (usually start[seqs]; a start that goes back or leaves the arrays takes
+        // none from the others)
+        if (ln < a.seq.seqs) claim(ln, first0, end0);
+        n = end0;
+        for (int s = ln + 32; s < a.seq.seqs; s += 32) {
+            int first, end;
+            claim(s, first, end);
+            n = max(n, end);
         }
         n = __reduce_max_sync(0xffffffffu, n);
         // what is wrong with any sequence is reported by the warp that has the least to do
@@ -124,29 +133,22 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
         long long k_at = 0, v_at = 0;
         bool there = true, stored = false;
         auto find_place = [&]() {
-            int b = 0;                                     // sequences that end at or before this row
-            for (int s = ln; s - ln < a.seq.seqs; s += 32)
-                b += __popc(__ballot_sync(0xffffffffu, s < a.seq.seqs && __ldcg(a.seq.start + s + 1) <= row));
-            SeqRange r = {0, 0, 0, false};
-            if (b < a.seq.seqs) r = seq_range(a.seq, b, a.cache.page);
-            there = r.ok && row >= r.first && row - r.first < r.n;
-            if (!there) {                                  // a row of no sequence, or starts that go back somewhere: look at all
-                unsigned found = 0;
-                for (int s0 = 0; s0 < a.seq.seqs && !found; s0 += 32) {
-                    SeqRange c = {0, 0, 0, false};
-                    if (s0 + ln < a.seq.seqs) c = seq_range(a.seq, s0 + ln, a.cache.page);
-                    found = __ballot_sync(0xffffffffu, c.ok && row >= c.first && row - c.first < c.n);
-                    if (found) {
-                        const int src = __ffs(found) - 1;
-                        b = s0 + src;
-                        r.first = __shfl_sync(0xffffffffu, c.first, src);
-                        r.n = __shfl_sync(0xffffffffu, c.n, src);
-                        r.length = __shfl_sync(0xffffffffu, c.length, src);
-                    }
-                }
-                there = found != 0;
+            // the sequence that claims this row (the first one, should there be several)
+            int end = end0, mine = row >= first0 && row < end0 ? ln : a.seq.seqs;
+            for (int s = ln + 32; s < a.seq.seqs; s += 32) {
+                int f, e;
+                claim(s, f, e);
+                if (mine == a.seq.seqs && row >= f && row < e) { mine = s; end = e; }
             }
-            const int slot = r.length - r.n + (row - r.first);
+            const int b = __reduce_min_sync(0xffffffffu, mine);
+            there = b < a.seq.seqs;
+            int slot = -1;
+            if (there) {
+                end = __shfl_sync(0xffffffffu, end, b & 31);
+                const int length = __ldcg(a.seq.length + b);
+                there = length_fits(a.seq, length, a.cache.page);
+                slot = length - end + row;
+            }
             bool bad = false;
             if (there && slot >= 0) {
                 const int index = quotient(slot, a.cache.page);
