@@ -213,11 +213,9 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
                         const float wu = INTER ? (2 * c < V ? w0[2 * c % V] : w1[2 * c % V]) : w0[c];
                         const float wv = INTER ? (2 * c + 1 < V ? w0[(2 * c + 1) % V] : w1[(2 * c + 1) % V]) : w1[c];
                         const int j = (INTER ? e[u][0] >> 1 : e[u][0]) + c;
-                        // (channels that do not turn add (+0)(-0) = -0, which changes nothing, a negative zero neither)
-                        const bool on = turned[u] && j < pairs;
-                        const float2 t = on ? turn[j] : make_float2(1.f, 0.f);
-                        cu[u][c] = wu * t.x; su[u][c] = on ? wu * t.y : -0.f;
-                        cv[u][c] = wv * t.x; sv[u][c] = on ? -wv * t.y : -0.f;
+                        const float2 t = turned[u] && j < pairs ? turn[j] : make_float2(1.f, 0.f);
+                        cu[u][c] = wu * t.x; su[u][c] = wu * t.y;
+                        cv[u][c] = wv * t.x; sv[u][c] = -wv * t.y;
                     }
                 }
             }
@@ -287,10 +285,11 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
                                 if (weight) { pu = mul2(pu, inv); if (!INTER) pv = mul2(pv, inv); }
                                 Pair qu = pu, qv = pv;
                                 if (INTER) { const float2 t = both_of(pu); qv = pair_of(t.y, t.x); }
-                                // (channels that do not turn: their neighbour, whatever it holds, plays no part)
+                                // (channels that do not turn: their neighbour, whatever it holds, plays no part.  sv is -0 there and
+                                // su +0; with these signs both products are -0, so that a negative zero stays one.)
                                 if (rot < D) {
                                     const bool t = turned[u] && (!INTER || (e[u][0] >> 1) + c < pairs);
-                                    qu = t ? qu : 0; qv = t ? qv : 0;
+                                    qu = t ? qu : pair_of(-0.f, -0.f); qv = t ? qv : pair_of(0.f, INTER ? -0.f : 0.f);
                                 }
                                 const float2 y0 = both_of(fma2(pu, cu2[u][c], mul2(qv, sv2[u][c])));
                                 const float2 y1 = INTER ? y0 : both_of(fma2(pv, cv2[u][c], mul2(qu, su2[u][c])));
@@ -323,7 +322,7 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
                         }
 #pragma unroll
                         for (int u = 0; u < NI; ++u) {
-                            const float pu = x[u][0] * inv, pv = x[u][1] * inv, qu = turned[u] ? pu : 0.f, qv = turned[u] ? pv : 0.f;
+                            const float pu = x[u][0] * inv, pv = x[u][1] * inv, qu = turned[u] ? pu : -0.f, qv = turned[u] ? pv : 0.f;
                             const float r0[1] = {fmaf(pu, cu[u][0], qv * sv[u][0])}, r1[1] = {fmaf(pv, cv[u][0], qu * su[u][0])};
                             res[u][0] = pack<1>(r0, T{}); res[u][1] = pack<1>(r1, T{});
                         }
