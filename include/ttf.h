@@ -371,7 +371,7 @@ typedef struct {
     const int* table;                /* [seqs, table_pages]                                                            */
     long long table_stride;          /* elements between the rows of the table: table_pages or more, or 0 (one for all) */
     int table_pages;
-    int seqs;
+    int seqs;                        /* at most 2^30                                                                   */
     int rows;                        /* capacity of the packed arrays                                                  */
 } ttf_sequences;
 

@@ -103,6 +103,7 @@ static int check_sequences(const ttf_sequences* s) {
     if (!s || s->seqs < 1 || s->rows < 1 || s->table_pages < 1) return TTF_ERR_INVALID_ARG;
     // (a stride of zero: all sequences have one list of pages)
     if (!s->start || !s->length || !s->table || (s->table_stride != 0 && s->table_stride < s->table_pages)) return TTF_ERR_INVALID_ARG;
+    if (s->seqs > 1 << 30) return TTF_ERR_UNSUPPORTED;     // (the kernels count 32 beyond them)
     return reachable(s->seqs, s->table_stride, s->table_pages, 1, 0, 0) ? TTF_OK : TTF_ERR_UNSUPPORTED;
 }
 static int check_cache(const ttf_cache* c) {
