@@ -14,6 +14,8 @@
 // sums are kept per lane until the end.  Warps, and the CTAs of a cluster that share the slots of long sequences, join their sums
 // through shared memory.
 //
+// P is rounded to bf16 for the second product, l adds up the weights before that (as in ttf_attend_tc.cu, with the same error).
+//
 // Values of slots that no row of the tile sees are zeroed in shared memory, whatever the page holds there.
 //
 // Every mbarrier wait is bounded: a warp whose wait runs out reports it and stops; what its copies in flight still write is waited

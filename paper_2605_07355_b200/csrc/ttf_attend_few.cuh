@@ -103,7 +103,8 @@ __device__ __forceinline__ void join_rows(const AttendArgs& a, JoinSpace<D>& jn,
 // how long it is.  Shares of long sequences stay above 2048 slots, so that the last CTAs to run are short against the call: 64
 // sequences of 500 to 16000 slots, 8 heads of 128: 230 / 206 / 187 / 200 us with 1 / 2 / 4 / 8; 64 of 4400: 197 / 181 / 183 / 205;
 // 64 of 500: 36 / 45 / 63 / 103 (what a CTA costs before its first and after its last block is not small against those).  Where
-// the CTAs do not fill the GPU shares go down to 128 slots: one sequence of 2760 slots 32 / 19 / 12.3 / 9.2 us.
+// the CTAs do not fill the GPU shares go down to 128 slots: one sequence of 2760 slots 32 / 19 / 12.3 / 9.2 us.  (What a sequence
+// may be is the width of its table: 64 sequences of 500 slots take 35 us with a table of 500 slots, 62 with 8192, 101 with 16384.)
 inline int few_split(const AttendArgs& a, long long ctas) {
     const long long slots = (long long)a.seq.table_pages * a.cache.page.d;
     const long long reach = (long long)a.window + a.seq.rows, longest = a.window > 0 && reach < slots ? reach : slots;

@@ -19,6 +19,8 @@
 // sums are kept per lane until the end.
 // Warps and the CTAs of a cluster, which share the slots of long sequences, join their sums through shared memory.
 //
+// P is rounded to bf16 for the second product, l adds up the weights before that (as in ttf_attend_tc.cu, with the same error).
+//
 // Slots that no row of the tile sees are fetched as zeros, whatever the page holds there.
 #include "ttf_paged.cuh"
 #include "ttf_attend_few.cuh"

@@ -20,9 +20,14 @@
 // softmax waits 600 for its scores and spends 40 on loading them, 290 on the maximum, 1000 on exponentials, sums and conversion;
 // the thread that issues is held 1390 of them by its twelve products (those of the scores are 64 slots wide and so read Q from
 // shared memory twice a block, 1.5 times what they multiply).  A CTA adds 6 us before its first scores and after its last.
-// 4096 new rows over 16384 slots, 32 heads of 128: 890 us, 1.08 PFLOP/s, about 1010 under the power cap.  Slower were: scores
-// handed over whole 1205, two threads a row 1022, one warp for both tiles' products 1330, an eighth of the exponentials on the
-// fp32 pipe 917; scores and sums issued by two threads a tile made no difference.
+// 4096 new rows over 16384 slots, 32 heads of 128: 1010 to 1025 us back to back, where the power cap holds the clock down (0.95
+// PFLOP/s), 900 in bursts of 20 ms (1.07).  In such bursts slower were: scores handed over whole 1205, two threads a row 1022, one
+// warp for both tiles' products 1330, an eighth of the exponentials on the fp32 pipe 917; scores and sums issued by two threads a
+// tile made no difference.
+//
+// Rounded to fewer bits: the weights P, to bf16, since the second product takes its operands in 16 bits.  Each is off by half a step
+// at most (2^-8 of its value), to either side; l adds up what they were before.  Against 64 bits the result is off by 0.0022 of its
+// size, an fp32 evaluation rounded once by 0.0017.  ex2.approx is within 2 steps of fp32.
 //
 // Few tiles over many slots: the CTAs of a cluster share the blocks, and each finishes a part of the rows from what all of them
 // send into its shared memory.

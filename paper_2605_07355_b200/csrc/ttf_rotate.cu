@@ -122,6 +122,7 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
                     } else axis = j < a.sec0 ? 0 : (j < a.sec0 + a.sec1 ? 1 : 2);
                 }
                 const double w = (double)__ldcg(a.pos + (long long)row * a.axes + axis) * ((double)__ldcg(a.freq + j) * 0.15915494309189533577);
+                // (what is left of the turn, half a turn at most, is rounded to fp32: the angle is off by pi 2^-25 at most)
                 float c, s;
                 sincospif((float)(2.0 * (w - rint(w))), &s, &c);
                 turn[j] = make_float2(c * a.factor, s * a.factor);
@@ -285,8 +286,8 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
                                 if (weight) { pu = mul2(pu, inv); if (!INTER) pv = mul2(pv, inv); }
                                 Pair qu = pu, qv = pv;
                                 if (INTER) { const float2 t = both_of(pu); qv = pair_of(t.y, t.x); }
-                                // (channels that do not turn: their neighbour, whatever it holds, plays no part.  sv is -0 there and
-                                // su +0; with these signs both products are -0, so that a negative zero stays one.)
+                                // (channels that do not turn: their neighbour, whatever it holds, plays no part.  Without a norm
+                                // sv is -0 there and su +0; with these signs both products are -0, and a negative zero stays one.)
                                 if (rot < D) {
                                     const bool t = turned[u] && (!INTER || (e[u][0] >> 1) + c < pairs);
                                     qu = t ? qu : pair_of(-0.f, -0.f); qv = t ? qv : pair_of(0.f, INTER ? -0.f : 0.f);
