@@ -53,3 +53,28 @@ def test_threads_that_begin_together(case):
     r = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
                        capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stdout[-500:] + r.stderr[-2000:]
+
+
+CAPTURE = """
+import torch
+import paper_2605_07355_b200 as P
+from tests.test_gpu_attend import Batch
+b = Batch([1], [6000], 16, 8, 1, {D}, "{dtype}", spare=0)
+args = b.on_device()
+out = torch.zeros_like(args[0])
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    P.ttf_attend(*args, b.scale, out=out)
+g.replay()
+assert P.ttf_paged_status() == 0
+assert torch.equal(P.ttf_attend(*args, b.scale, out=torch.zeros_like(out)), out) and bool((out != 0).any())
+"""
+
+
+@pytest.mark.parametrize("D,dtype", [(128, "bf16"), (256, "bf16"), (128, "f32"), (256, "f32")])
+def test_a_capture_whose_clusters_the_device_is_asked_about(D, dtype):
+    """the first call of a process, captured, with so long a sequence that sixteen CTAs may share it"""
+    r = subprocess.run([sys.executable, "-c", CAPTURE.format(D=D, dtype=dtype)],
+                       cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout[-500:] + r.stderr[-2000:]
