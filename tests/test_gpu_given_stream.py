@@ -27,6 +27,7 @@ def calls():
     k, v = torch.randn(rows, 2, 64, device="cuda").bfloat16(), torch.randn(rows, 2, 64, device="cuda").bfloat16()
     pos, freq = torch.arange(rows, dtype=torch.int32, device="cuda"), torch.rand(32, device="cuda")
     ck, cv = bk.clone(), bv.clone()
+    torch.cuda.synchronize()                                # (the calls run on other streams than the one that makes the inputs)
 
     def cut(out, m):
         return [out[0][:m], out[1], out[2][:m]]
@@ -53,6 +54,15 @@ def calls():
 NAMES = ["compress", "batch", "mean", "segment", "query", "restore", "histogram", "stats", "rotate", "append", "attend"]
 
 
+def alone(f, stream):
+    """the outputs of a call that has the GPU to itself (and the stream's own scratch is there after it)"""
+    out = f(stream)
+    torch.cuda.synchronize()                                # (the copies are made on the current stream)
+    out = [t.clone() for t in out]
+    torch.cuda.synchronize()
+    return out
+
+
 def whole(t):
     return torch.empty(t.untyped_storage().nbytes(), dtype=torch.uint8, device="cuda")
 
@@ -62,8 +72,7 @@ def whole(t):
 def test_memory_that_the_current_stream_still_writes(name, as_int):
     f, side = calls()[name], torch.cuda.Stream()
     given = side.cuda_stream if as_int else side
-    want = [t.clone() for t in f(given)]                    # (and the stream's own scratch)
-    torch.cuda.synchronize()
+    want = alone(f, given)
     junk = [whole(t) for t in f(None)]
     torch.cuda.synchronize()
     torch.cuda._sleep(20_000_000)                           # some 10 ms, and then all of it is written
@@ -79,8 +88,7 @@ def test_memory_that_the_current_stream_still_writes(name, as_int):
 @pytest.mark.parametrize("name", NAMES)
 def test_memory_that_the_current_stream_still_reads(name):
     f, side = calls()[name], torch.cuda.Stream()
-    want = [t.clone() for t in f(side)]
-    torch.cuda.synchronize()
+    want = alone(f, side)
     got = f(side)
     torch.cuda.current_stream().wait_stream(side)
     torch.cuda._sleep(20_000_000)
