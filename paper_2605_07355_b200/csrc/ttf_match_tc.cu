@@ -228,10 +228,10 @@ k_match_tc(const __grid_constant__ ClipMaps<G> maps, int F, int H, int W, int C,
     float win[S::WIN];                                     // this row's window of dot products
     float na = 0.f, nb = 0.f;                              // squared norm of source row m / of candidate row et
 
+    int issued = 0;                                        // the producing lane: stages whose copies it has issued
     if (warp == 0) {
         // ---- producer: one lane issues the tile copies of every stage ----------------------------------------
         if (lane == 0) {
-            int issued = 0;
             const uint64_t once = l2_evict_first_policy();
             for (int it = 0; it < nst; ++it) {
                 const int s = it % S::STAGES;
@@ -248,12 +248,6 @@ k_match_tc(const __grid_constant__ ClipMaps<G> maps, int F, int H, int W, int C,
                 issued = it + 1;
             }
             trace_mark_any(asrc.hdr, 12, false); trace_mark_any(asrc.hdr, 12, true);   // all copies issued
-            if (*(volatile int*)&s_err) {
-                // copies already issued still land in this CTA's shared memory: wait (bounded) for the stages that
-                // nobody consumed before the CTA is allowed to exit
-                for (int it = issued > S::STAGES ? issued - S::STAGES : 0; it < issued; ++it)
-                    mbar_wait(&bar_full[it % S::STAGES], (it / S::STAGES) & 1, wait_limit);
-            }
         }
     } else if (warp == 1) {
         // ---- MMA issuer: one lane, four K = 16 steps per stage -----------------------------------------------
@@ -450,10 +444,18 @@ k_match_tc(const __grid_constant__ ClipMaps<G> maps, int F, int H, int W, int C,
 
     // ---- teardown: every role is done with tensor memory before its owner frees it --------------------------
     tc_fence_before();
-    __syncthreads();
+    __syncthreads();                                       // (from here on nobody gives up any more)
     trace_mark(asrc.hdr, 2, true);
+    if (issued && s_err) {
+        // copies already issued still land in this CTA's shared memory: wait (bounded) for the stages that nobody consumed before
+        // the CTA is allowed to exit
+        for (int it = issued > S::STAGES ? issued - S::STAGES : 0; it < issued; ++it)
+            mbar_wait(&bar_full[it % S::STAGES], (it / S::STAGES) & 1, wait_limit);
+    }
     if (warp == 1) {
         tc_fence_after();
+        if (s_err) mbar_wait(&bar_acc, 0, wait_limit);     // products in flight end before their accumulators are given back
+        __syncwarp();
         tmem_dealloc(tmem, tmem_cols);
     }
     if (tid == 0 && s_err) report_give_up(asrc.hdr, asrc.begins);
