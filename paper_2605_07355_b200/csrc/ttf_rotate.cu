@@ -16,6 +16,7 @@
 // Rows are dealt out to the warps by the number that only the device knows, so worst-case buffers cost nothing.
 #include "ttf_paged.cuh"
 
+#include <climits>
 #include <type_traits>
 
 namespace ttf {
@@ -73,30 +74,31 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
         turned[u] = in[u][0] && e[u][0] < rot;
     }
     pdl_wait();
-    int n = a.rows;
-    // append: the rows [first, end) that sequence s claims (none, if they do not lie within the arrays)
-    auto claim = [&](int s, int& first, int& end) {
-        const int f = __ldcg(a.seq.start + s), e = __ldcg(a.seq.start + s + 1);
-        const bool in_rows = f >= 0 && e > f && e <= a.rows;
-        first = in_rows ? f : 0; end = in_rows ? e : 0;
-    };
-    [[maybe_unused]] int first0 = 0, end0 = 0;             // those of this lane's one of the first 32 sequences
+    int n = a.rows, beyond = 0;
+    // append: every step-th sequence's rows [first, end), one per lane
+    [[maybe_unused]] const int step0 = (a.seq.seqs + 31) >> 5;
+    [[maybe_unused]] int first0 = INT_MAX, end0 = 0;
+    auto sequence_rows = [&](int s, int& first, int& end) { first = __ldcg(a.seq.start + s); end = __ldcg(a.seq.start + s + 1); };
+    auto claims = [&](int first, int end, int row) { return first >= 0 && first <= row && row < end && end <= a.rows; };
     if (APPEND) {
-        // rows up to the last one that any sequence claims (usually start[seqs]; a start that goes back or leaves the arrays takes
-        // none from the others)
-        if (ln < a.seq.seqs) claim(ln, first0, end0);
-        n = end0;
-        for (int s = ln + 32; s < a.seq.seqs; s += 32) {
-            int first, end;
-            claim(s, first, end);
-            n = max(n, end);
-        }
-        n = __reduce_max_sync(0xffffffffu, n);
-        // what is wrong with any sequence is reported by the warp that has the least to do
+        if (ln * step0 < a.seq.seqs) sequence_rows(ln * step0, first0, end0);
+        // rows up to the last one that is claimed; of more than 32 sequences up to the last start, which is that where none goes back
+        // (one more load than up to 32 need: append_streams 11.2 us so, 11.9 with the last start throughout)
+        if (step0 == 1) n = __reduce_max_sync(0xffffffffu, claims(first0, end0, first0) ? end0 : 0);
+        else n = min(n, max(0, __ldcg(a.seq.start + a.seq.seqs)));
+        // The warp that has the least to do looks at all sequences, and reports what is wrong with any.  Rows beyond n that a sequence
+        // claims all the same are its own.
         if (blockIdx.x == gridDim.x - 1 && warp == kRotThreads / 32 - 1) {
             bool bad = false;
-            for (int s = ln; s < a.seq.seqs; s += 32) bad |= !seq_range(a.seq, s, a.cache.page).ok;
+            int last = 0;
+            for (int s = ln; s < a.seq.seqs; s += 32) {
+                int first, end;
+                sequence_rows(s, first, end);
+                bad |= !seq_range(a.seq, s, a.cache.page).ok;
+                if (end > first && claims(first, end, first)) last = max(last, end);
+            }
             if (bad) report_paged(a.hdr, 2);
+            beyond = max(0, __reduce_max_sync(0xffffffffu, last) - n);
         }
     } else if (a.count) n = min(n, max(0, __ldcg(a.count)));
 
@@ -105,9 +107,19 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
     if (n > 0 && n < warps) parts = min(min(warps / n, (heads + per_warp - 1) / per_warp), kRotParts);
     const int units = n * parts;
     // (without a sign: units may be as many as 2^31 - 1, and a warp counts one step beyond them)
-    for (unsigned at = warp * gridDim.x + blockIdx.x; at < (unsigned)units; at += warps) {
-        const int unit = (int)at, row = parts > 1 ? unit / parts : unit, part = unit - row * parts;
-        const int h0 = parts > 1 ? heads * part / parts : 0, h1 = parts > 1 ? heads * (part + 1) / parts : heads;
+    for (unsigned at = warp * gridDim.x + blockIdx.x; ; at += warps) {
+        int row, h0 = 0, h1 = heads;
+        if (at < (unsigned)units) {
+            const int unit = (int)at;
+            row = parts > 1 ? unit / parts : unit;
+            if (parts > 1) {
+                const int part = unit - row * parts;
+                h0 = heads * part / parts; h1 = heads * (part + 1) / parts;
+            }
+        } else if (APPEND && beyond > 0) {
+            row = n + --beyond;
+            at -= warps;
+        } else break;
 
         bool have = false;
         auto make_turns = [&]() {                          // cosine and sine of the row's pairs, for all lanes
@@ -134,18 +146,29 @@ k_rotate(const __grid_constant__ RotateArgs a, int llanes)
         long long k_at = 0, v_at = 0;
         bool there = true, stored = false;
         auto find_place = [&]() {
-            // the sequence that claims this row (the first one, should there be several)
-            int end = end0, mine = row >= first0 && row < end0 ? ln : a.seq.seqs;
-            for (int s = ln + 32; s < a.seq.seqs; s += 32) {
-                int f, e;
-                claim(s, f, e);
-                if (mine == a.seq.seqs && row >= f && row < e) { mine = s; end = e; }
+            // the sequence that claims this row: 32 starts at a time, as long as they do not go back
+            int lo = 0, step = step0, first = first0, end = end0;
+            while (step > 1) {
+                const unsigned upto = __ballot_sync(0xffffffffu, first <= row);
+                lo += upto ? (31 - __clz(upto)) * step : 0;
+                const int left = min(step, a.seq.seqs - lo);
+                step = (left + 31) >> 5;
+                first = INT_MAX;
+                if (ln * step < left) sequence_rows(lo + ln * step, first, end);
             }
-            const int b = __reduce_min_sync(0xffffffffu, mine);
-            there = b < a.seq.seqs;
+            unsigned found = __ballot_sync(0xffffffffu, claims(first, end, row));
+            if (!found && step0 > 1)                       // a row of no sequence, or starts that go back somewhere: look at all
+                for (lo = 0; lo < a.seq.seqs; lo += 32) {
+                    first = INT_MAX;
+                    if (lo + ln < a.seq.seqs) sequence_rows(lo + ln, first, end);
+                    found = __ballot_sync(0xffffffffu, claims(first, end, row));
+                    if (found) break;
+                }
+            const int src = __ffs(found) - 1, b = lo + src;
+            there = found != 0;
             int slot = -1;
             if (there) {
-                end = __shfl_sync(0xffffffffu, end, b & 31);
+                end = __shfl_sync(0xffffffffu, end, src);
                 const int length = __ldcg(a.seq.length + b);
                 there = length_fits(a.seq, length, a.cache.page);
                 slot = length - end + row;
